@@ -223,8 +223,8 @@ def run(s):
                                      prefix_pages=s["prefix"], prefix_L=s["P"], k_scale=s["k_scale"], v_scale=s["v_scale"], out=s["out"], lse_out=s["lse"],
                                      workspace=s["ws"]["space"])
     return gr.gr_logits_adjust(s["logits"], s["level"], prefix=s["prefix"], scores=s["scores"], history=s["history"], cu_history=s["cu"],
-                               max_history=s["max_history"], repetition=s["repetition"], frequency=s["frequency"], presence=s["presence"], bias=s["bias"],
-                               allowed=s["allowed"], allowed_row=s["allowed_row"], out=s["out"])
+                               repetition=s["repetition"], frequency=s["frequency"], presence=s["presence"], bias=s["bias"], allowed=s["allowed"],
+                               allowed_row=s["allowed_row"], out=s["out"])
 
 
 def _values(pages):
@@ -236,7 +236,7 @@ def _plain_map(s):
     seq, new, page, free, table = s["seq"].long(), s["new"].long(), s["page"], s["free"], s["table"]
     B, max_pages = table.shape
     first, last = (seq + page - 1) // page, (seq + new + page - 1) // page
-    need = last - first
+    need = torch.where(seq + new <= table.shape[1] * page, last - first, 0)
     cu = torch.cat([new.new_zeros(1), new.cumsum(0)])
     off = need.cumsum(0) - need
     served = (seq + new <= max_pages * page) & (cu[1:] <= s["total"]) & ((need == 0) | (off + need <= free.numel()))
