@@ -10,7 +10,8 @@
  *   3. the move of every surviving beam's own decode cache to its new slot, in place (Section 5.1) - or, moving no
  *      bytes, the update of a slot table that the attention follows (gr_beam_slot_update, gr_beam_attn_slots).
  * Beside the step: the prefill that fills the shared cache (gr_prefill_attn), the step's attention over a shared
- * cache stored in FP8 (gr_beam_attn_fp8kv), an item step for callers that cannot allocate
+ * cache stored in FP8 (gr_beam_attn_fp8kv), a prompt cache in pages with a prefix that requests share (gr_page_map, gr_page_write,
+ * gr_beam_attn_paged), penalties, biases and masks on the logits (gr_logits_adjust), an item step for callers that cannot allocate
  * (gr_beam_select_noalloc), and a few diagnostics used by the benchmark (gr_diag_*).
  *
  * Conventions for every entry point
@@ -278,6 +279,140 @@ gr_status gr_beam_reorder(int32_t B, int32_t W, int32_t ND, int32_t Hkv, int32_t
 gr_status gr_beam_slot_update(int32_t B, int32_t W, int32_t ND, int32_t u, const int32_t* parent, const int32_t* slot_in,
                               int32_t* slot_out, void* stream);
 gr_status gr_beam_attn_slots(const gr_attn_params* p, const int32_t* slot, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * A prompt cache in pages.  gr_beam_attn reads a prompt cache that is packed for one batch.  A server whose requests come and go keeps the
+ * prompts in pages of a pool instead, and a prefix that all of them share (an instruction, a context) once:
+ *   gr_page_map          pages are handed out of a free list for the new tokens of every request; block tables and slot map
+ *   gr_page_write        K/V rows of new tokens (as prefill produced them) into their slots, in bf16 or as FP8 codes
+ *   gr_beam_attn_paged   the decode step's attention over such pages
+ * A pool is [n_pages, page_size, Hkv, d] for K and the same for V; page_size is a power of two from 16 to 1024.  Slot s of a pool is
+ * token s % page_size of page s / page_size.  Token t of request b lies in page block_table[b, t / page_size].
+ * ------------------------------------------------------------------------------------------------ */
+enum {
+  GR_KV_BF16 = 0,
+  GR_KV_FP8 = 1                   /* OCP FP8 E4M3 codes, uint8; the value of an element is code * scale, one scale per tensor */
+};
+
+/* gr_page_map - request b has seq_lens[b] tokens in its pages and gets new_lens[b] more (negative lengths count as 0).  Where its last page is full
+ * (or it has none) it gets fresh pages, free_pages[0], free_pages[1], ... in the order of the requests, which are written into its row of
+ * block_table from entry ceil(seq_lens[b] / page_size) on; other entries are left as they were.  A request is served whole or not at all: it is
+ * not served, gets no pages and keeps its length, if it would need more than max_pages pages, if its new tokens do not fit into the slot map, or
+ * if too few pages are left for it (then no request behind it that needs a page is served).
+ *   lens_out  tokens after the call
+ *   cu_new    exclusive sums of new_lens (they stop at 2^31 - 1); the new tokens of request b are rows cu_new[b] .. cu_new[b+1] - 1
+ *   slot      slot of every new token; -1 for tokens of requests that are not served, of a page number outside [0, n_pages), and
+ *             behind the last token
+ *   taken     {pages taken from the free list, requests with new tokens that were not served}
+ * The same inputs give the same tables, so a host that knows the lengths can follow the free list without reading anything back.  Only enqueues on
+ * `stream`.  The outputs must not overlap the inputs or each other.  Supported: B <= 4096; max_pages * page_size, n_pages * page_size and
+ * total_new below 2^31 - 1024.  Errors: INVALID_ARG, UNSUPPORTED, HIP. */
+typedef struct {
+  int32_t B, page_size;
+  int32_t max_pages;              /* entries of a row of block_table                                   */
+  int32_t n_free, n_pages;        /* entries of free_pages; pages of the pool                          */
+  int64_t total_new;              /* entries of slot (normally the sum of new_lens)                    */
+  const int32_t* seq_lens;        /* int32 [B]                                                         */
+  const int32_t* new_lens;        /* int32 [B]                                                         */
+  const int32_t* free_pages;      /* int32 [n_free]                                                    */
+  int32_t*       block_table;     /* int32 [B, max_pages], entries of fresh pages are written          */
+  int32_t*       lens_out;        /* int32 [B]                                                         */
+  int32_t*       cu_new;          /* int32 [B+1]                                                       */
+  int32_t*       slot;            /* int32 [total_new]                                                 */
+  int32_t*       taken;           /* int32 [2]                                                         */
+} gr_page_map_params;
+gr_status gr_page_map(const gr_page_map_params* p, void* stream);
+
+/* gr_page_write - row t of k and v (Hkv * d elements, rows k_stride and v_stride elements apart: they may be parts of a fused projection's rows) goes to slot
+ * slot[t] of the pools.  Rows whose slot is outside [0, n_pages * page_size) are not written; which row is kept where two have the same slot is
+ * not defined.  GR_KV_FP8: code = the E4M3 value nearest to x / scale (ties to even; the division is rounded to fp32 first), values beyond
+ * +-448 saturate, NaN stays NaN.  Only enqueues on `stream`.  Supported: Hkv * d and the strides multiples of 8; T and n_pages * page_size
+ * below 2^31.  k, v and the pools 16-byte aligned.  Errors: INVALID_ARG, UNSUPPORTED, HIP. */
+typedef struct {
+  int64_t T;                      /* rows                                                              */
+  int32_t Hkv, d, page_size, n_pages;
+  int32_t kv_type;                /* GR_KV_*: element type of the pools                                */
+  float   k_scale, v_scale;       /* GR_KV_FP8: positive and finite                                    */
+  int64_t k_stride, v_stride;     /* elements from a row to the next, at least Hkv * d                 */
+  const void*    k;               /* bf16                                                              */
+  const void*    v;               /* bf16                                                              */
+  const int32_t* slot;            /* int32 [T]                                                         */
+  void*          k_pages;         /* bf16 or uint8 [n_pages, page_size, Hkv, d]                        */
+  void*          v_pages;
+} gr_page_write_params;
+gr_status gr_page_write(const gr_page_write_params* p, void* stream);
+
+/* gr_beam_attn_paged - gr_beam_attn over a prompt cache in pages.  The keys of beam w of request b are, in this order, the prefix_L tokens that all
+ * requests share (pages prefix_pages[0], prefix_pages[1], ...), the request's own seq_lens[b] tokens (pages block_table[b, 0], ...), and
+ * the beam's own u tokens, as for gr_beam_attn (with `slot` as for gr_beam_attn_slots, or NULL).  Any part may be empty; a beam
+ * without a single key gets out = 0 and lse = -inf.  The prefix is read and multiplied once for the rows of all requests where that is
+ * less work than with each request's rows by themselves.
+ * What a table holds beyond a request's pages is not read; a page number outside [0, n_pages) is read as page 0, and a length outside [0, max_L] as the
+ * nearer end.  Slots of a page behind a request's last token may hold anything.
+ * GR_KV_FP8: pools of E4M3 codes, scales applied as in gr_beam_attn_fp8kv.
+ * Supported: d in {64, 128}; Hq % Hkv == 0; 0 <= u <= ND; prefix_L a multiple of page_size; n_pages * page_size and prefix_L + max_L below 2^31;
+ * Hkv * d <= 65536; W * Hq/Hkv < 2^22.  bf16 tensors and pools 16-byte aligned; finite values in the slots that are read; |v| * 2^8 * (number of keys) below 2^128.
+ * Workspace (device, 256-byte aligned, contents unspecified before and after): partial results of segments, where a row's keys are split.
+ * Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE_TOO_SMALL, HIP. */
+typedef struct {
+  int32_t B, W, Hq, Hkv, d;
+  int32_t ND, u;                  /* own-token capacity of a beam, and valid own tokens                */
+  int32_t page_size, max_pages, n_pages;
+  int32_t prefix_L;               /* tokens of the shared prefix                                       */
+  int32_t max_L;                  /* host copy of max_b seq_lens[b]; at most max_pages * page_size     */
+  int32_t kv_type;                /* GR_KV_*: element type of the pools                                */
+  float   sm_scale;               /* positive and finite                                               */
+  float   k_scale, v_scale;       /* GR_KV_FP8: positive and finite                                    */
+  const void*    q;               /* bf16 [B, W, Hq, d]                                                */
+  const void*    k_pages;         /* bf16 or uint8 [n_pages, page_size, Hkv, d]                        */
+  const void*    v_pages;
+  const int32_t* prefix_pages;    /* int32 [prefix_L / page_size]; may be NULL when prefix_L == 0      */
+  const int32_t* block_table;     /* int32 [B, max_pages]; may be NULL when max_L == 0                 */
+  const int32_t* seq_lens;        /* int32 [B]; may be NULL when max_L == 0                            */
+  const void*    k_unshared;      /* bf16 [B, W, ND, Hkv, d]; may be NULL when u == 0                  */
+  const void*    v_unshared;
+  const int32_t* slot;            /* int32 [B, W, ND] or NULL                                          */
+  void*          out;             /* bf16 [B, W, Hq, d]                                                */
+  float*         lse_out;         /* fp32 [B, W, Hq] or NULL                                           */
+} gr_attn_paged_params;
+
+/* Bytes of workspace for these shapes; pointers, scales, u and ND are not looked at (0 is possible).  Host only. */
+size_t gr_beam_attn_paged_workspace_bytes(const gr_attn_paged_params* p);
+gr_status gr_beam_attn_paged(const gr_attn_paged_params* p, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * gr_logits_adjust - penalties, biases and masks on the logits of an item step, in front of gr_beam_select.
+ *
+ * For every live beam w of request b (scores[b, w] > -inf; every beam where scores is NULL) and token v, with x = logits[b, w, v]:
+ *     c  = number of rows h of the request's history with h[t] == prefix[b, w, t] for t < step and h[step] == v
+ *          (items that the user has seen and that this token would continue; with depth = 1, step = 0: how often the token occurred)
+ *     y  = c > 0 ? (x > 0 ? x / repetition[b] : x * repetition[b]) - (frequency[b] * c + presence[b]) : x
+ *     y += bias[b, v]
+ *     y  = -inf where the mask row of the beam has bit v clear, whatever x was
+ * in fp32.  Rows of dead beams are left as they are.  `out` is `logits` itself (in place; rows without a bias or a mask are then changed at the counted
+ * tokens alone) or does not overlap it.  Any of the parts may be absent (NULL).  repetition is positive.  History rows whose
+ * token lies outside [0, V) count nothing.
+ * Supported: 1 <= V <= 32768; depth <= 8.  Only enqueues on `stream`.  Errors: INVALID_ARG, UNSUPPORTED, HIP.
+ * ------------------------------------------------------------------------------------------------ */
+typedef struct {
+  int32_t B, W, V, depth, step;   /* 0 <= step < depth                                                 */
+  int32_t n_history;              /* rows of history                                                   */
+  int32_t bias_rows;              /* 1: one bias for all requests; B: one for each                     */
+  int32_t n_allowed;              /* rows of allowed                                                   */
+  const float*    logits;         /* fp32 [B, W, V]                                                    */
+  float*          out;            /* fp32 [B, W, V]                                                    */
+  const float*    scores;         /* fp32 [B, W] or NULL                                               */
+  const int32_t*  prefix;         /* int32 [B, W, depth]; needed with a history when step > 0          */
+  const int32_t*  history;        /* int32 [n_history, depth]                                          */
+  const int32_t*  cu_history;     /* int32 [B+1]: request b owns rows cu[b] .. cu[b+1] - 1             */
+  const float*    repetition;     /* fp32 [B] or NULL (1)                                              */
+  const float*    frequency;      /* fp32 [B] or NULL (0)                                              */
+  const float*    presence;       /* fp32 [B] or NULL (0)                                              */
+  const float*    bias;           /* fp32 [bias_rows, V] or NULL                                       */
+  const uint32_t* allowed;        /* [n_allowed, ceil(V / 32)] or NULL; bit v % 32 of word v / 32      */
+  const int32_t*  allowed_row;    /* int32 [B, W] row of allowed for each beam (outside [0, n_allowed): nothing is forbidden), or NULL (row 0) */
+} gr_logits_adjust_params;
+gr_status gr_logits_adjust(const gr_logits_adjust_params* p, void* stream);
 
 /* ------------------------------------------------------------------------------------------------
  * Diagnostics: the rates this GPU really sustains, reported by the benchmark next to the datasheet peaks

@@ -6,6 +6,10 @@ The calls have the names and meaning of the C ABI in include/gr.h:
     gr_item_mask_build   valid-item mask blob from the sorted item table (load time)
     gr_beam_select       masked log-softmax + beam score accumulation + top-W selection
     gr_beam_reorder      in-place move of the surviving beams' own KV cache to their new slots
+    gr_page_map          pages of a pool handed out for new tokens: block tables and slot map
+    gr_page_write        K/V rows of new tokens into their slots of the pools (bf16 or FP8 codes)
+    gr_beam_attn_paged   beam attention over a prompt cache in pages, behind a prefix that all requests share
+    gr_logits_adjust     penalties for seen items, biases and masks on the logits of an item step
 
 This module only marshals arguments (torch CUDA tensors -> device pointers, current stream ->
 hipStream_t), for the calls of the decode loop in native code (csrc/gr_bind.cpp).  Every step of the path runs in the
@@ -21,7 +25,8 @@ from . import build as _build
 __all__ = ["load_library", "gr_beam_attn", "gr_beam_attn_fp8kv", "gr_prefill_attn", "gr_item_mask_build", "gr_beam_select", "gr_beam_select_noalloc", "gr_beam_reorder",
            "gr_status_string",
            "attn_workspace_bytes", "select_workspace_bytes", "GrError", "GR_SELECT_FORCE_DENSE", "LIB_PATH",
-           "gr_diag_stream_read", "gr_diag_mfma_loop", "gr_diag_attn_plan", "gr_diag_issue_loop", "gr_diag_issue_loop_lds", "gr_beam_attn_slots", "gr_beam_slot_update"]
+           "gr_diag_stream_read", "gr_diag_mfma_loop", "gr_diag_attn_plan", "gr_diag_issue_loop", "gr_diag_issue_loop_lds", "gr_beam_attn_slots", "gr_beam_slot_update",
+           "gr_page_map", "gr_page_write", "gr_beam_attn_paged", "attn_paged_workspace_bytes", "gr_logits_adjust"]
 
 LIB_PATH = _build.LIB_PATH
 GR_SELECT_FORCE_DENSE = 1
@@ -62,6 +67,12 @@ class _SelectParams(ctypes.Structure):
                 ("prefix_in", ctypes.c_void_p), ("range_in", ctypes.c_void_p), ("parent_out", ctypes.c_void_p),
                 ("token_out", ctypes.c_void_p), ("scores_out", ctypes.c_void_p), ("prefix_out", ctypes.c_void_p),
                 ("range_out", ctypes.c_void_p), ("item_index_out", ctypes.c_void_p)]
+
+
+class _AttnPagedParams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "W", "Hq", "Hkv", "d", "ND", "u", "page_size", "max_pages", "n_pages", "prefix_L", "max_L", "kv_type")] + [
+        ("sm_scale", ctypes.c_float), ("k_scale", ctypes.c_float), ("v_scale", ctypes.c_float)] + [
+        (n, ctypes.c_void_p) for n in ("q", "k_pages", "v_pages", "prefix_pages", "block_table", "seq_lens", "k_unshared", "v_unshared", "slot", "out", "lse_out")]
 
 
 def load_library(path: str = None):
@@ -117,6 +128,13 @@ def load_library(path: str = None):
     lib.gr_diag_mfma_flops.argtypes = [ctypes.c_int32, ctypes.c_int32]
     lib.gr_beam_reorder.restype = ctypes.c_int32
     lib.gr_beam_reorder.argtypes = [ctypes.c_int32] * 6 + [ctypes.c_void_p] * 4
+    for name in ("gr_page_map", "gr_page_write", "gr_logits_adjust"):
+        getattr(lib, name).restype = ctypes.c_int32
+        getattr(lib, name).argtypes = [ctypes.c_void_p, ctypes.c_void_p]
+    lib.gr_beam_attn_paged.restype = ctypes.c_int32
+    lib.gr_beam_attn_paged.argtypes = [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]
+    lib.gr_beam_attn_paged_workspace_bytes.restype = ctypes.c_size_t
+    lib.gr_beam_attn_paged_workspace_bytes.argtypes = [ctypes.c_void_p]
     _lib, _native = lib, None            # (the marshalling module binds to this library at its next call)
     return lib
 
@@ -134,7 +152,8 @@ def _marshal():
         loader.exec_module(native)
         native.bind(*(ctypes.cast(getattr(lib, f), ctypes.c_void_p).value for f in (
             "gr_beam_attn", "gr_beam_attn_slots", "gr_beam_attn_fp8kv", "gr_beam_attn_workspace_bytes", "gr_prefill_attn", "gr_beam_select",
-            "gr_beam_select_noalloc", "gr_beam_select_workspace_bytes", "gr_beam_reorder", "gr_beam_slot_update")), _current_stream_handle)
+            "gr_beam_select_noalloc", "gr_beam_select_workspace_bytes", "gr_beam_reorder", "gr_beam_slot_update",
+            "gr_page_map", "gr_page_write", "gr_beam_attn_paged", "gr_beam_attn_paged_workspace_bytes", "gr_logits_adjust")), _current_stream_handle)
         _native = native
     return _native
 
@@ -327,6 +346,82 @@ def gr_beam_slot_update(parent, slot_in, u, ND, out=None, stream=None):
     rc = native.slot_update(parent, slot_in, u, ND, out, stream)
     if rc != 0:
         raise GrError(rc, "gr_beam_slot_update")
+    return out
+
+
+def gr_page_map(seq_lens, new_lens, free_pages, block_table, page_size, n_pages, total_new, out=None, stream=None):
+    """Pages for new tokens.  int32 CUDA tensors: seq_lens [B] tokens that the requests have in their pages, new_lens [B] tokens they get, free_pages [n] page
+    numbers to hand out, block_table [B, max_pages], whose entries of fresh pages are written.  total_new: tokens in all (host integer).
+    `out` may hold preallocated int32 tensors under the keys lens [B] (tokens after the call), cu_new [B+1], slot [total_new], taken [2] (pages
+    taken, requests not served).  Returns that dict.  Enqueues on `stream`."""
+    native = _native or _marshal()
+    out = {} if out is None else out
+    if any(out.get(k) is None for k in ("lens", "cu_new", "slot", "taken")):
+        B = block_table.shape[0]
+        for k, n in (("lens", B), ("cu_new", B + 1), ("slot", int(total_new)), ("taken", 2)):
+            if out.get(k) is None:
+                out[k] = _empty(n, "int32", block_table.device, stream)
+    rc = native.page_map(seq_lens, new_lens, free_pages, block_table, page_size, n_pages, total_new, out["lens"], out["cu_new"], out["slot"], out["taken"], stream)
+    if rc != 0:
+        raise GrError(rc, "gr_page_map")
+    return out
+
+
+def _empty(shape, dtype, device, stream):
+    """An output that the wrapper allocates; like a workspace of its own, it belongs to the stream that the kernels run on."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=getattr(torch, dtype), device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=getattr(torch, dtype), device=device)
+
+
+def gr_page_write(k, v, slot, k_pages, v_pages, k_scale=1.0, v_scale=1.0, stream=None):
+    """K/V rows into their slots.  k, v bf16 [T,Hkv,d], rows contiguous and any stride apart; slot int32 [T] (outside the pool: not written);
+    k_pages, v_pages [n_pages,page_size,Hkv,d]: bf16, or uint8 for E4M3 codes of x / scale.  Enqueues on `stream`."""
+    rc = (_native or _marshal()).page_write(k, v, slot, k_pages, v_pages, k_scale, v_scale, stream)
+    if rc != 0:
+        raise GrError(rc, "gr_page_write")
+
+
+def attn_paged_workspace_bytes(B, W, Hq, Hkv, d, max_L, prefix_L=0, fp8=False, page_size=16) -> int:
+    """Workspace bytes of gr_beam_attn_paged.  Without page_size: enough for pages of any size."""
+    p = _AttnPagedParams()
+    p.B, p.W, p.Hq, p.Hkv, p.d, p.max_L, p.prefix_L, p.kv_type, p.page_size = B, W, Hq, Hkv, d, int(max_L), int(prefix_L), int(bool(fp8)), int(page_size)
+    return int(load_library().gr_beam_attn_paged_workspace_bytes(ctypes.byref(p)))
+
+
+def gr_beam_attn_paged(q, k_pages, v_pages, block_table, seq_lens, k_unshared, v_unshared, u, sm_scale, max_L, prefix_pages=None, prefix_L=0, k_scale=1.0,
+                       v_scale=1.0, slot=None, out=None, lse_out=None, workspace=None, stream=None):
+    """Beam attention over a prompt cache in pages.  q bf16 [B,W,Hq,d]; k/v_pages [n_pages,page_size,Hkv,d], bf16 or uint8 (E4M3 codes, value = code * scale);
+    block_table int32 [B,max_pages]; seq_lens int32 [B]; k/v_unshared bf16 [B,W,ND,Hkv,d] (None: no own tokens, u = 0); `slot` as for gr_beam_attn_slots.
+    prefix_pages int32 [prefix_L/page_size]: pages of the tokens in front that all requests share.  max_L (of seq_lens) and prefix_L are host
+    integers.  Returns (out bf16 [B,W,Hq,d], lse fp32 [B,W,Hq] or None).  Enqueues on `stream` (default: current)."""
+    native = _native or _marshal()
+    if out is None:
+        out = _empty(q.shape, "bfloat16", q.device, stream)
+    args = (q, k_pages, v_pages, block_table, seq_lens, k_unshared, v_unshared, u, sm_scale, max_L, prefix_pages, prefix_L, k_scale, v_scale, slot, out, lse_out)
+    rc = native.attn_paged(*args, workspace, stream)
+    if rc > 0:                                   # no workspace was given: so many bytes are needed
+        rc = native.attn_paged(*args, _scratch(rc, q.device, stream), stream)
+    if rc != 0:
+        raise GrError(rc, "gr_beam_attn_paged")
+    return out, lse_out
+
+
+def gr_logits_adjust(logits, step, prefix=None, scores=None, history=None, cu_history=None, repetition=None, frequency=None, presence=None, bias=None,
+                     allowed=None, allowed_row=None, out=None, stream=None):
+    """Penalties, biases and masks on logits fp32 [B,W,V], in front of gr_beam_select.  history int32 [n,depth] (items that the requests' users have seen, request b's
+    in rows cu_history[b] .. cu_history[b+1]-1; depth 1, step 0: plain tokens); prefix int32 [B,W,depth]: the beams' tokens so far; repetition,
+    frequency, presence fp32 [B]; bias fp32 [V] or [B,V]; allowed int32 [n,ceil(V/32)]: rows of bits, allowed_row int32 [B,W] says which is a beam's (-1:
+    none; without it row 0 is everybody's).  scores fp32 [B,W]: rows of beams at -inf are left as they are.  out=None: a new tensor, in which
+    dead beams' rows are unspecified; out=logits: in place.  Returns out.  Enqueues on `stream`."""
+    native = _native or _marshal()
+    if out is None:
+        out = _empty(logits.shape, "float32", logits.device, stream)
+    rc = native.adjust(logits, step, prefix, scores, history, cu_history, repetition, frequency, presence, bias, allowed, allowed_row, out, stream)
+    if rc != 0:
+        raise GrError(rc, "gr_logits_adjust")
     return out
 
 

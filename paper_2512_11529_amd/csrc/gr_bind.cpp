@@ -3,8 +3,11 @@
 // than the kernels of a small batch; here it is about one.  Host code only; the library is reached through the addresses that
 // bind() is given, so whatever libgr.so the package has loaded is the one that runs.
 #include <Python.h>
+#include <c10/core/DeviceGuard.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <initializer_list>
+#include <optional>
 #include <string>
 
 #include "gr.h"
@@ -21,6 +24,11 @@ decltype(&gr_beam_select_noalloc) p_select_noalloc = nullptr;
 decltype(&gr_beam_select_workspace_bytes) p_select_ws = nullptr;
 decltype(&gr_beam_reorder) p_reorder = nullptr;
 decltype(&gr_beam_slot_update) p_slot_update = nullptr;
+decltype(&gr_page_map) p_page_map = nullptr;
+decltype(&gr_page_write) p_page_write = nullptr;
+decltype(&gr_beam_attn_paged) p_attn_paged = nullptr;
+decltype(&gr_beam_attn_paged_workspace_bytes) p_attn_paged_ws = nullptr;
+decltype(&gr_logits_adjust) p_adjust = nullptr;
 
 struct Error {};        // a Python exception is set
 
@@ -96,6 +104,32 @@ void* pointer(PyObject* o) { return (void*)(uintptr_t)(unsigned long long)intege
 void count(Py_ssize_t n, Py_ssize_t want) {
   if (n != want) { PyErr_SetString(PyExc_TypeError, "wrong number of arguments"); throw Error(); }
 }
+
+// The tensors' common GPU, which becomes the current one until the end of the call (whatever was current), and the stream: the given one, which has to be of
+// that GPU, or its current one.
+struct OnDevice {
+  std::optional<c10::DeviceGuard> guard;
+  c10::Device device{c10::kCPU};
+  void add(const char* name, const at::Tensor& t) {
+    if (!guard) { device = t.device(); guard.emplace(device); return; }
+    if (t.device() == device) return;
+    PyErr_Format(PyExc_ValueError, "%s: expected a tensor on %s, got one on %s", name, device.str().c_str(), t.device().str().c_str());
+    throw Error();
+  }
+  void* stream(PyObject* o) const {
+    if (o != Py_None) {
+      PyObject* at = PyObject_GetAttrString(o, "device_index");
+      if (!at) throw Error();
+      const long long index = integer(at);
+      Py_DECREF(at);
+      if (index != device.index()) {
+        PyErr_Format(PyExc_ValueError, "stream: expected one of %s", device.str().c_str());
+        throw Error();
+      }
+    }
+    return stream_of(o);
+  }
+};
 
 template <class F>
 PyObject* guarded(F&& f) {
@@ -250,10 +284,177 @@ PyObject* slot_update(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// bind(addresses of the ten entry points in the order of their declaration above, callable that returns the current stream's handle)
+// page_map(seq_lens, new_lens, free_pages, block_table, page_size, n_pages, total_new, lens, cu_new, slot, taken, stream) -> status
+PyObject* page_map(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    count(n, 12);
+    OnDevice on;
+    auto ints = [&](PyObject* o, const char* name, c10::IntArrayRef shape) {
+      const at::Tensor& t = tensor(o, at::kInt, name, shape);
+      on.add(name, t);
+      return (int32_t*)t.data_ptr();
+    };
+    const at::Tensor& table = tensor_nd(a[3], at::kInt, "block_table", 2);
+    on.add("block_table", table);
+    const int64_t B = table.size(0), free_pages = tensor_nd(a[2], at::kInt, "free_pages", 1).size(0);
+    gr_page_map_params p{};
+    p.B = (int32_t)B; p.max_pages = (int32_t)table.size(1); p.page_size = (int32_t)integer(a[4]); p.n_pages = (int32_t)integer(a[5]);
+    p.n_free = (int32_t)free_pages; p.total_new = integer(a[6]);
+    p.seq_lens = ints(a[0], "seq_lens", {B}); p.new_lens = ints(a[1], "new_lens", {B}); p.free_pages = ints(a[2], "free_pages", {free_pages});
+    p.block_table = (int32_t*)table.data_ptr();
+    p.lens_out = ints(a[7], "lens", {B}); p.cu_new = ints(a[8], "cu_new", {B + 1}); p.slot = ints(a[9], "slot", {p.total_new}); p.taken = ints(a[10], "taken", {2});
+    void* stream = on.stream(a[11]);
+    return status_of([&] { return p_page_map(&p, stream); });
+  });
+}
+
+// Rows [T, Hkv, d] that are whole in memory and one stride apart; -> that stride
+int64_t rows_of(PyObject* o, const char* name, const at::Tensor** t) {
+  *t = THPVariable_Check(o) ? &THPVariable_Unpack(o) : nullptr;
+  const bool dense = *t && (*t)->is_cuda() && (*t)->dim() == 3 && ((*t)->numel() == 0 || (((*t)->size(2) == 1 || (*t)->stride(2) == 1) && ((*t)->size(1) == 1 || (*t)->stride(1) == (*t)->size(2))));
+  if (!dense) {
+    PyErr_Format(PyExc_TypeError, "%s: expected a CUDA tensor [rows, KV heads, head size] of contiguous rows", name);
+    throw Error();
+  }
+  if ((*t)->scalar_type() != at::kBFloat16) {
+    PyErr_Format(PyExc_TypeError, "%s: expected torch.bfloat16, got %s", name, dtype_text((*t)->scalar_type()));
+    throw Error();
+  }
+  return (*t)->size(0) > 1 ? (*t)->stride(0) : (*t)->size(1) * (*t)->size(2);
+}
+const at::Tensor& pool(PyObject* o, const char* name, bool* fp8) {
+  *fp8 = THPVariable_Check(o) && THPVariable_Unpack(o).scalar_type() == at::kByte;
+  return tensor_nd(o, *fp8 ? at::kByte : at::kBFloat16, name, 4);
+}
+
+// page_write(k, v, slot, k_pages, v_pages, k_scale, v_scale, stream) -> status
+PyObject* page_write(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    count(n, 8);
+    OnDevice on;
+    const at::Tensor *k, *v;
+    gr_page_write_params p{};
+    p.k_stride = rows_of(a[0], "k", &k);
+    p.v_stride = rows_of(a[1], "v", &v);
+    on.add("k", *k);
+    on.add("v", *v);
+    if (v->sizes() != k->sizes()) {
+      PyErr_Format(PyExc_ValueError, "v: expected shape %s, got %s", shape_text(k->sizes()).c_str(), shape_text(v->sizes()).c_str());
+      throw Error();
+    }
+    bool fp8;
+    const at::Tensor& kp = pool(a[3], "k_pages", &fp8);
+    const at::ScalarType type = fp8 ? at::kByte : at::kBFloat16;
+    tensor(a[3], type, "k_pages", {kp.size(0), kp.size(1), k->size(1), k->size(2)});
+    const at::Tensor& vp = tensor(a[4], type, "v_pages", kp.sizes());
+    const at::Tensor& slot = tensor(a[2], at::kInt, "slot", {k->size(0)});
+    on.add("slot", slot);
+    on.add("k_pages", kp);
+    on.add("v_pages", vp);
+    p.T = k->size(0); p.Hkv = (int32_t)k->size(1); p.d = (int32_t)k->size(2); p.n_pages = (int32_t)kp.size(0); p.page_size = (int32_t)kp.size(1);
+    p.kv_type = fp8 ? GR_KV_FP8 : GR_KV_BF16;
+    p.k_scale = (float)real(a[5]); p.v_scale = (float)real(a[6]);
+    p.k = k->data_ptr(); p.v = v->data_ptr(); p.slot = (const int32_t*)slot.data_ptr(); p.k_pages = kp.data_ptr(); p.v_pages = vp.data_ptr();
+    void* stream = on.stream(a[7]);
+    return status_of([&] { return p_page_write(&p, stream); });
+  });
+}
+
+// attn_paged(q, k_pages, v_pages, block_table, seq_lens, k_own | None, v_own | None, u, sm_scale, max_L, prefix_pages | None, prefix_L, k_scale, v_scale,
+//            slot | None, out, lse | None, workspace | None, stream) -> status (<= 0), or the workspace bytes that the call needs when none was given
+PyObject* attn_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    count(n, 19);
+    OnDevice on;
+    const at::Tensor& q = tensor_nd(a[0], at::kBFloat16, "q", 4);
+    on.add("q", q);
+    const int64_t B = q.size(0), W = q.size(1), Hq = q.size(2), d = q.size(3);
+    auto given = [&](PyObject* o, at::ScalarType type, const char* name, c10::IntArrayRef shape) -> void* {
+      if (o == Py_None) return nullptr;
+      const at::Tensor& t = tensor(o, type, name, shape);
+      on.add(name, t);
+      return t.data_ptr();
+    };
+    bool fp8;
+    const at::Tensor& kp = pool(a[1], "k_pages", &fp8);
+    const at::ScalarType type = fp8 ? at::kByte : at::kBFloat16;
+    const int64_t pages = kp.size(0), page = kp.size(1), Hkv = kp.size(2);
+    gr_attn_paged_params p{};
+    p.k_pages = given(a[1], type, "k_pages", {pages, page, Hkv, d});
+    p.v_pages = given(a[2], type, "v_pages", {pages, page, Hkv, d});
+    const at::Tensor& table = tensor_nd(a[3], at::kInt, "block_table", 2);
+    p.block_table = (const int32_t*)given(a[3], at::kInt, "block_table", {B, table.size(1)});
+    p.seq_lens = (const int32_t*)given(a[4], at::kInt, "seq_lens", {B});
+    const long long prefix_L = integer(a[11]), max_L = integer(a[9]);
+    if (prefix_L < 0 || prefix_L >= (1ll << 31) || max_L < 0 || max_L >= (1ll << 31)) { PyErr_SetString(PyExc_ValueError, "prefix_L and max_L: expected numbers of tokens"); throw Error(); }
+    p.prefix_pages = page > 0 && prefix_L % page == 0 ? (const int32_t*)given(a[10], at::kInt, "prefix_pages", {prefix_L / page}) : nullptr;
+    const int64_t ND = a[5] == Py_None ? 0 : tensor_nd(a[5], at::kBFloat16, "k_unshared", 5).size(2);
+    p.k_unshared = given(a[5], at::kBFloat16, "k_unshared", {B, W, ND, Hkv, d});
+    p.v_unshared = given(a[6], at::kBFloat16, "v_unshared", {B, W, ND, Hkv, d});
+    p.slot = (const int32_t*)given(a[14], at::kInt, "slot", {B, W, ND});
+    p.out = given(a[15], at::kBFloat16, "out", {B, W, Hq, d});
+    p.lse_out = (float*)given(a[16], at::kFloat, "lse_out", {B, W, Hq});
+    p.B = (int32_t)B; p.W = (int32_t)W; p.Hq = (int32_t)Hq; p.Hkv = (int32_t)Hkv; p.d = (int32_t)d; p.ND = (int32_t)ND; p.u = (int32_t)integer(a[7]);
+    p.page_size = (int32_t)page; p.max_pages = (int32_t)table.size(1); p.n_pages = (int32_t)pages; p.prefix_L = (int32_t)prefix_L; p.max_L = (int32_t)max_L;
+    p.kv_type = fp8 ? GR_KV_FP8 : GR_KV_BF16;
+    p.sm_scale = (float)real(a[8]); p.k_scale = (float)real(a[12]); p.v_scale = (float)real(a[13]);
+    p.q = q.data_ptr();
+    size_t ws_bytes;
+    void* ws = const_cast<void*>(any_tensor(a[17], &ws_bytes));
+    if (a[17] != Py_None) on.add("workspace", THPVariable_Unpack(a[17]));
+    void* stream = on.stream(a[18]);
+    if (a[17] == Py_None) {
+      const size_t need = p_attn_paged_ws(&p);
+      if (need > 0) return workspace_wanted(need);
+    }
+    return status_of([&] { return p_attn_paged(&p, ws, ws_bytes, stream); });
+  });
+}
+
+// adjust(logits, step, prefix | None, scores | None, history | None, cu_history | None, repetition | None, frequency | None, presence | None, bias | None,
+//        allowed | None, allowed_row | None, out, stream) -> status
+PyObject* adjust(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    count(n, 14);
+    OnDevice on;
+    const at::Tensor& logits = tensor_nd(a[0], at::kFloat, "logits", 3);
+    on.add("logits", logits);
+    const int64_t B = logits.size(0), W = logits.size(1), V = logits.size(2);
+    auto given = [&](PyObject* o, at::ScalarType type, const char* name, c10::IntArrayRef shape) -> void* {
+      if (o == Py_None) return nullptr;
+      const at::Tensor& t = tensor(o, type, name, shape);
+      on.add(name, t);
+      return t.data_ptr();
+    };
+    gr_logits_adjust_params p{};
+    const int64_t rows = a[4] == Py_None ? 0 : tensor_nd(a[4], at::kInt, "history", 2).size(0);
+    const int64_t depth = a[4] != Py_None ? tensor_nd(a[4], at::kInt, "history", 2).size(1) : a[2] != Py_None ? tensor_nd(a[2], at::kInt, "prefix", 3).size(2) : integer(a[1]) + 1;
+    p.logits = (const float*)logits.data_ptr();
+    p.prefix = (const int32_t*)given(a[2], at::kInt, "prefix", {B, W, depth});
+    p.scores = (const float*)given(a[3], at::kFloat, "scores", {B, W});
+    p.history = (const int32_t*)given(a[4], at::kInt, "history", {rows, depth});
+    p.cu_history = (const int32_t*)given(a[5], at::kInt, "cu_history", {B + 1});
+    p.repetition = (const float*)given(a[6], at::kFloat, "repetition", {B});
+    p.frequency = (const float*)given(a[7], at::kFloat, "frequency", {B});
+    p.presence = (const float*)given(a[8], at::kFloat, "presence", {B});
+    const bool of_request = a[9] != Py_None && THPVariable_Check(a[9]) && THPVariable_Unpack(a[9]).dim() == 2;
+    p.bias = (const float*)(of_request ? given(a[9], at::kFloat, "bias", {B, V}) : given(a[9], at::kFloat, "bias", {V}));
+    p.bias_rows = of_request ? (int32_t)B : 1;
+    const int64_t masks = a[10] == Py_None ? 0 : tensor_nd(a[10], at::kInt, "allowed", 2).size(0);
+    p.allowed = (const uint32_t*)given(a[10], at::kInt, "allowed", {masks, (V + 31) / 32});
+    p.allowed_row = (const int32_t*)given(a[11], at::kInt, "allowed_row", {B, W});
+    p.out = (float*)given(a[12], at::kFloat, "out", {B, W, V});
+    p.B = (int32_t)B; p.W = (int32_t)W; p.V = (int32_t)V; p.depth = (int32_t)depth; p.step = (int32_t)integer(a[1]);
+    p.n_history = (int32_t)rows; p.n_allowed = (int32_t)masks;
+    void* stream = on.stream(a[13]);
+    return status_of([&] { return p_adjust(&p, stream); });
+  });
+}
+
+// bind(addresses of the fifteen entry points in the order of their declaration above, callable that returns the current stream's handle)
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded([&]() -> PyObject* {
-    count(n, 11);
+    count(n, 16);
     p_attn = (decltype(p_attn))pointer(a[0]);
     p_attn_slots = (decltype(p_attn_slots))pointer(a[1]);
     p_attn_fp8kv = (decltype(p_attn_fp8kv))pointer(a[2]);
@@ -264,8 +465,13 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
     p_select_ws = (decltype(p_select_ws))pointer(a[7]);
     p_reorder = (decltype(p_reorder))pointer(a[8]);
     p_slot_update = (decltype(p_slot_update))pointer(a[9]);
-    Py_INCREF(a[10]);
-    Py_XSETREF(current_stream, a[10]);
+    p_page_map = (decltype(p_page_map))pointer(a[10]);
+    p_page_write = (decltype(p_page_write))pointer(a[11]);
+    p_attn_paged = (decltype(p_attn_paged))pointer(a[12]);
+    p_attn_paged_ws = (decltype(p_attn_paged_ws))pointer(a[13]);
+    p_adjust = (decltype(p_adjust))pointer(a[14]);
+    Py_INCREF(a[15]);
+    Py_XSETREF(current_stream, a[15]);
     Py_RETURN_NONE;
   });
 }
@@ -275,6 +481,10 @@ PyMethodDef methods[] = {{"attn", (PyCFunction)(void*)attn, METH_FASTCALL, nullp
                          {"select", (PyCFunction)(void*)select, METH_FASTCALL, nullptr},
                          {"reorder", (PyCFunction)(void*)reorder, METH_FASTCALL, nullptr},
                          {"slot_update", (PyCFunction)(void*)slot_update, METH_FASTCALL, nullptr},
+                         {"page_map", (PyCFunction)(void*)page_map, METH_FASTCALL, nullptr},
+                         {"page_write", (PyCFunction)(void*)page_write, METH_FASTCALL, nullptr},
+                         {"attn_paged", (PyCFunction)(void*)attn_paged, METH_FASTCALL, nullptr},
+                         {"adjust", (PyCFunction)(void*)adjust, METH_FASTCALL, nullptr},
                          {"bind", (PyCFunction)(void*)bind, METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "gr_bind", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

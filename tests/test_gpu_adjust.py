@@ -1,0 +1,187 @@
+"""GPU: penalties, biases and masks on logits against the definition in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2512_11529_amd as gr
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def make(seed, B, W, V, depth, step, hist, penalties="rfp", bias=None, masks=0, dead=0.0, families=6):
+    g = np.random.default_rng(seed)
+    n = [int(x) for x in (g.integers(0, hist + 1, B) if B > 1 else [hist])]
+    cu = np.cumsum([0] + n).astype(np.int32)
+    items = g.integers(0, V, (cu[-1], depth)).astype(np.int32)
+    items[:, :-1] %= families
+    if cu[-1]:
+        items[g.random(cu[-1]) < 0.3] = items[g.integers(0, cu[-1])]
+        items[g.random(cu[-1]) < 0.05, step] = g.choice([-1, V, 2 ** 31 - 1, -2 ** 31])      # no tokens at all
+    prefix = g.integers(0, families, (B, W, depth)).astype(np.int32)
+    logits = (3 * g.standard_normal((B, W, V))).astype(np.float32)
+    scores = -g.random((B, W)).astype(np.float32)
+    scores[g.random((B, W)) < dead] = -np.inf
+    f32 = lambda lo, hi: (lo + (hi - lo) * g.random(B)).astype(np.float32)
+    s = dict(step=step, logits=logits, prefix=prefix, scores=scores if dead else None, history=items if penalties else None, cu_history=cu if penalties else None,
+             repetition=f32(0.8, 1.6) if "r" in penalties else None, frequency=f32(-0.2, 0.5) if "f" in penalties else None, presence=f32(-0.2, 0.7) if "p" in penalties else None,
+             bias=None if bias is None else g.standard_normal((V,) if bias == 1 else (B, V)).astype(np.float32), allowed=None, allowed_row=None)
+    if masks:
+        s["allowed"] = g.integers(-2 ** 31, 2 ** 31, (masks, -(-V // 32))).astype(np.int32)
+        s["allowed"][0] = 0 if masks > 1 else s["allowed"][0]                                  # a mask that forbids everything
+        s["allowed_row"] = g.integers(-1, masks + 1, (B, W)).astype(np.int32)                  # -1 and `masks`: nothing is forbidden
+    return s
+
+
+def definition(s):
+    """Result, and the sum of the sizes of what was added up."""
+    x = s["logits"].astype(np.float64)
+    B, W, V = x.shape
+    y, size = x.copy(), np.abs(x)
+    step = s["step"]
+    penal = any(s[k] is not None for k in ("repetition", "frequency", "presence"))
+    for b in range(B):
+        r, f, p = (float(s[k][b]) if s[k] is not None else d for k, d in (("repetition", 1.0), ("frequency", 0.0), ("presence", 0.0)))
+        h = s["history"][s["cu_history"][b]:s["cu_history"][b + 1]] if s["history"] is not None else np.zeros((0, step + 1), np.int32)
+        for w in range(W):
+            c = np.zeros(V)
+            if penal and len(h):
+                t = h[(h[:, :step] == s["prefix"][b, w, :step]).all(1), step]
+                np.add.at(c, t[(t >= 0) & (t < V)], 1)
+            k = c > 0
+            y[b, w, k] = np.where(x[b, w, k] > 0, x[b, w, k] / r, x[b, w, k] * r) - (f * c[k] + p)
+            size[b, w, k] = np.abs(np.where(x[b, w, k] > 0, x[b, w, k] / r, x[b, w, k] * r)) + 2 * np.abs(f * c[k]) + np.abs(p)
+    if s["bias"] is not None:
+        add = (s["bias"] if s["bias"].ndim == 1 else s["bias"][:, None, :]).astype(np.float64)
+        y, size = y + add, size + np.abs(add)
+    if s["allowed"] is not None:
+        bits = np.unpackbits(s["allowed"].view(np.uint8), axis=1, bitorder="little")[:, :V]
+        row = s["allowed_row"] if s["allowed_row"] is not None else np.zeros((B, W), np.int32)
+        for b in range(B):
+            for w in range(W):
+                if 0 <= row[b, w] < len(bits):
+                    y[b, w, bits[row[b, w]] == 0] = -np.inf
+    return y, size
+
+
+def check(s, inplace):
+    t = {k: (torch.from_numpy(np.ascontiguousarray(v)).to(DEV) if isinstance(v, np.ndarray) else v) for k, v in s.items()}
+    logits, step = t.pop("logits"), t.pop("step")
+    before = logits.clone()
+    out = logits if inplace else torch.full_like(logits, 77.0)
+    got = gr.gr_logits_adjust(logits, step, out=out, **t)
+    assert got is out
+    torch.cuda.synchronize()
+    want, size = definition(s)
+    got = out.cpu().numpy()
+    live = np.ones(want.shape[:2], bool) if s["scores"] is None else s["scores"] > -np.inf
+    # five roundings at most (a quotient, a product, its sum, a difference, the bias), each of half a step of something no larger than `size`
+    inf = np.isinf(want)
+    assert np.array_equal(np.isneginf(got)[live], inf[live])
+    assert np.array_equal(np.isposinf(got)[live], np.zeros_like(inf[live]))
+    fine = live[..., None] & ~inf
+    with np.errstate(invalid="ignore"):
+        err = np.abs(got.astype(np.float64) - want)
+    assert (err[fine] <= 5 * 2.0 ** -24 * size[fine] + 1e-42).all(), err[fine].max()
+    left = (before.cpu().numpy() if inplace else np.full_like(got, 77.0))[~live]
+    assert np.array_equal(got[~live], left)
+    if not inplace:
+        assert torch.equal(logits.view(torch.int32), before.view(torch.int32))       # (as bits: there may be NaN)
+
+
+@pytest.mark.parametrize("inplace", [False, True])
+@pytest.mark.parametrize("V", [1, 3, 31, 32, 33, 255, 1000, 4097, 8192, 8193, 12003, 32768])
+def test_vocabularies(V, inplace):
+    for k, (bias, masks) in enumerate(((None, 0), (1, 0), (None, 5), (2, 5))):
+        check(make(V + k, 3, 5, V, 3, 1, 200, bias=bias, masks=masks, dead=0.2), inplace)
+
+
+@pytest.mark.parametrize("inplace", [False, True])
+@pytest.mark.parametrize("depth,step", [(1, 0), (3, 0), (3, 1), (3, 2), (8, 7), (8, 3), (2, 0)])
+def test_levels(depth, step, inplace):
+    check(make(depth * 9 + step, 4, 6, 500, depth, step, 300, families=2), inplace)
+    check(make(depth * 9 + step, 2, 3, 40, depth, step, 300, bias=1, masks=3, families=1), inplace)
+
+
+@pytest.mark.parametrize("inplace", [False, True])
+@pytest.mark.parametrize("penalties", ["r", "f", "p", "rf", "", "rfp"])
+def test_parts(penalties, inplace):
+    for bias, masks in ((None, 0), (1, 0), (None, 2)):
+        check(make(len(penalties), 3, 4, 300, 1, 0, 100, penalties=penalties, bias=bias, masks=masks), inplace)
+
+
+@pytest.mark.parametrize("inplace", [False, True])
+@pytest.mark.parametrize("hist", [0, 1, 255, 256, 257, 8192, 8193, 20000])
+def test_history_lengths(hist, inplace):
+    check(make(hist, 1, 2, 700, 1, 0, hist), inplace)
+    check(make(hist + 1, 2, 3, 50, 2, 1, hist, families=2, bias=1), inplace)
+
+
+def test_one_mask_for_everybody_and_rows_outside():
+    for inplace in (False, True):
+        s = make(5, 2, 4, 333, 1, 0, 0, penalties="", masks=1)
+        s["allowed_row"] = None
+        check(s, inplace)
+
+
+@pytest.mark.parametrize("inplace", [False, True])
+def test_infinities_and_nan(inplace):
+    s = make(6, 2, 3, 256, 1, 0, 400, bias=1, masks=2)
+    x = s["logits"]
+    x[0, 0, :64] = -np.inf                                               # stays -inf whatever is added
+    bits = np.unpackbits(s["allowed"].view(np.uint8), axis=1, bitorder="little")
+    s["allowed_row"][1] = 1
+    x[1][:, bits[1][:256] == 0] = np.nan                                 # forbidden: -inf, not NaN
+    x[1, 0, bits[1][:256] == 0] = np.inf
+    check(s, inplace)
+    s["bias"] = None
+    check(s, inplace)
+    s = make(7, 1, 1, 64, 1, 0, 0, penalties="")
+    s["bias"] = np.zeros(64, np.float32)
+    s["logits"][0, 0, 5] = np.nan                                        # allowed: NaN stays
+    t = torch.from_numpy(s["logits"]).to(DEV)
+    y = gr.gr_logits_adjust(t, 0, bias=torch.from_numpy(s["bias"]).to(DEV))
+    assert torch.isnan(y).sum() == 1 and torch.isnan(y[0, 0, 5])
+
+
+def test_counts_are_bounded_by_the_history_given():
+    # sums that claim more rows than there are stay inside
+    s = make(8, 2, 3, 100, 1, 0, 50)
+    s["cu_history"] = np.array([0, len(s["history"]), 10 ** 9], np.int32)
+    t = {k: (torch.from_numpy(v).to(DEV) if isinstance(v, np.ndarray) else v) for k, v in s.items()}
+    logits, step = t.pop("logits"), t.pop("step")
+    got = gr.gr_logits_adjust(logits, step, **t)
+    s["cu_history"] = np.array([0, len(s["history"]), len(s["history"])], np.int32)
+    want, size = definition(s)
+    assert (np.abs(got.cpu().numpy() - want) <= 5 * 2.0 ** -24 * size).all()
+
+
+def test_same_bits_every_time_and_in_a_graph():
+    s = make(9, 3, 40, 5000, 3, 1, 900, bias=1, masks=4)
+    t = {k: (torch.from_numpy(v).to(DEV) if isinstance(v, np.ndarray) else v) for k, v in s.items()}
+    logits, step = t.pop("logits"), t.pop("step")
+    want = gr.gr_logits_adjust(logits, step, **t)
+    out = torch.zeros_like(logits)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        gr.gr_logits_adjust(logits, step, out=out, **t)
+    for _ in range(3):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+        assert torch.equal(gr.gr_logits_adjust(logits, step, **t), want)
+
+
+def test_on_another_stream():
+    side = torch.cuda.Stream()
+    logits = torch.zeros((2, 3, 64), device=DEV)
+    bias = torch.zeros(64, device=DEV)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(2_000_000)
+        bias.fill_(3.0)
+    got = gr.gr_logits_adjust(logits, 0, bias=bias, stream=side)
+    torch.cuda.synchronize()
+    assert (got == 3.0).all()
