@@ -9,6 +9,7 @@
 //     128 or 256 rows share their keys: the rows of one (request, KV head) pair share all of them (W * g rows), the rows of ALL requests
 //     share the prefix.  Where a request's rows leave most of a workgroup empty, part 0 of the launch packs all requests' rows against the prefix and
 //     part 1 takes each request's own pages; a second kernel joins the partials.  Else a row walks the whole list by itself.
+//   - Where a request's rows of a KV head are few, 32 of them meet the keys in a workgroup whose wavefronts share out the keys and not the rows.
 #include <type_traits>
 #include "gr_attn_tile.hpp"
 
@@ -55,10 +56,20 @@ __device__ __forceinline__ P* scalar(P* p) {
   return (P*)(uintptr_t)((uint64_t)hi << 32 | lo);
 }
 
+// The kernel's arguments, read where this stands and not before: what only late code needs takes no scalar registers through the loop.
+typedef const __attribute__((address_space(4))) PagedCtx* LateArgs;
+__device__ __forceinline__ LateArgs late_args() {
+  LateArgs a = (LateArgs)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(a));
+  return a;
+}
+
 constexpr int paged_lds_bytes(int d, int mwg) { return 4 * KT * d * 2 + (mwg == 256 ? mwg * d * 2 : 0) + kSegPages * 4; }
 
-template <int D, int NWAVES, bool KV8>
-__global__ void __launch_bounds__(NWAVES * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) k_paged_attn(PagedCtx c) {
+// One workgroup of NWAVES wavefronts and as many blocks of 32 rows.  SHARED: rows of all requests against the prefix (part 0), without own tokens; else rows of one
+// request against its whole list (part 1).
+template <int D, int NWAVES, bool KV8, bool SHARED>
+__device__ __forceinline__ void tile_rows(const PagedCtx& c, const unsigned id) {
   using T = AttnTile<D, 1>;
   constexpr int NT = NWAVES * 64, MWG = NWAVES * 32;
   constexpr int PPR = D / 8;                     // 16-byte pieces of a bf16 row
@@ -81,21 +92,16 @@ __global__ void __launch_bounds__(NWAVES * 64) __attribute__((amdgpu_waves_per_e
 
   // ---- the unit: a block of rows and a segment of their keys.  Workgroups are dealt round-robin to the 8 XCDs: ids congruent mod 8 share an L2, and the
   // row blocks that read the same keys get consecutive slots of one XCD.
-  const bool shared = blockIdx.x < c.grid0;
-  // (field by field: a reference to one part or the other is a copy in memory, and what comes from there is no scalar)
-  auto of = [&](auto a, auto b) { return shared ? a : b; };
-  const int M = of(c.part0.M, c.part1.M), ns = of(c.part0.ns, c.part1.ns);
-  const unsigned MB = (unsigned)of(c.part0.MB, c.part1.MB);
-  const uint32_t inv_ns = of(c.part0.inv_ns, c.part1.inv_ns);
-  const unsigned id = blockIdx.x - of(0u, c.grid0), place = id >> 3;
-  const unsigned nth = div_by(place, MB, of(c.part0.inv_mb, c.part1.inv_mb));
-  const int group = (int)(nth * 8 + (id & 7u)), mbi = (int)(place - nth * MB);
-  if (group >= of(c.part0.groups, c.part1.groups)) return;
-  const unsigned gq = div_by((unsigned)group, (unsigned)ns, inv_ns);
+  const PagedPart pt = SHARED ? c.part0 : c.part1;
+  const int M = pt.M, ns = pt.ns;
+  const unsigned place = id >> 3, nth = div_by(place, (unsigned)pt.MB, pt.inv_mb);
+  const int group = (int)(nth * 8 + (id & 7u)), mbi = (int)(place - nth * (unsigned)pt.MB);
+  if (group >= pt.groups) return;
+  const unsigned gq = div_by((unsigned)group, (unsigned)ns, pt.inv_ns);
   const int sp = group - (int)gq * ns;
-  const unsigned bu = shared ? 0u : div_by(gq, (unsigned)c.Hkv, c.inv_hkv);
-  const unsigned kvh = shared ? gq : gq - bu * (unsigned)c.Hkv;
-  const int L = __builtin_amdgcn_readfirstlane(shared || c.max_L == 0 ? 0 : min(max(c.lens[bu], 0), c.max_L));
+  const unsigned bu = SHARED ? 0u : div_by(gq, (unsigned)c.Hkv, c.inv_hkv);
+  const unsigned kvh = SHARED ? gq : gq - bu * (unsigned)c.Hkv;
+  const int L = __builtin_amdgcn_readfirstlane(SHARED || c.max_L == 0 ? 0 : min(max(c.lens[bu], 0), c.max_L));
 
   // ---- Q: the workgroup's rows come into LDS like K tiles, rows past the last one as that one (their columns are dropped)
   auto dma = [&](uint32_t lds_addr, const char* gbase, uint32_t off) {
@@ -103,8 +109,7 @@ __global__ void __launch_bounds__(NWAVES * 64) __attribute__((amdgpu_waves_per_e
   };
   const uint32_t lds_0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint16_t*)smem;
   const int beam_wg = __builtin_amdgcn_readfirstlane(small_div(mbi * MWG, c.rcp_g));
-  const size_t head_wg = ((size_t)bu * (unsigned)c.W + (unsigned)beam_wg) * (unsigned)c.Hq + kvh * (unsigned)c.g;      // of the workgroup's first beam
-  const uint16_t* q_b = scalar(c.q + head_wg * D);
+  const uint16_t* q_b = scalar(c.q + (((size_t)bu * (unsigned)c.W + (unsigned)beam_wg) * (unsigned)c.Hq + kvh * (unsigned)c.g) * D);
 #pragma unroll
   for (int i = 0; i < MWG / RPC / NWAVES; i++) {
     const int ch = i * NWAVES + wave_u, rl = ch * RPC + lane / PPR, r = min(mbi * MWG + rl, M - 1), beam = small_div(r, c.rcp_g);
@@ -112,15 +117,15 @@ __global__ void __launch_bounds__(NWAVES * 64) __attribute__((amdgpu_waves_per_e
         (uint32_t)((beam - beam_wg) * c.Hq + (r - beam * c.g)) * (D * 2) + (uint32_t)(((lane % PPR) ^ T::swz_k(rl)) * 16));
   }
 
-  const int front = shared ? c.prefix : c.own_prefix, keys = front + L;        // tokens of the list
-  int chunk = (int)div_by((unsigned)keys + (unsigned)ns - 1u, (unsigned)ns, inv_ns);
+  const int front = SHARED ? c.prefix : c.own_prefix, keys = front + L;        // tokens of the list
+  int chunk = (int)div_by((unsigned)keys + (unsigned)ns - 1u, (unsigned)ns, pt.inv_ns);
   chunk = (chunk + KT - 1) / KT * KT;
   const int seg0 = min(keys, sp * chunk), seg1 = min(keys, seg0 + chunk);
   const int ntiles = (seg1 - seg0 + KT - 1) / KT, tl = ntiles - 1;
   const int flip = tl & 1;
   // the segment that takes the beams' own tokens: the first, or the last where it has fewer tiles
   const int own_sp = max(0, keys - (ns - 1) * chunk + KT - 1) / KT < chunk / KT ? ns - 1 : 0;
-  const bool own_stage = !shared && c.u > 0 && sp == own_sp;
+  const bool own_stage = !SHARED && c.u > 0 && sp == own_sp;
 
   // ---- page numbers of the segment; one outside the pool is read as page 0
   const int mask = (1 << c.shift) - 1, page0 = seg0 >> c.shift, n_seg = ntiles > 0 ? ((seg1 - 1) >> c.shift) - page0 + 1 : 0;
@@ -149,8 +154,8 @@ __global__ void __launch_bounds__(NWAVES * 64) __attribute__((amdgpu_waves_per_e
   const uint32_t v_piece = KV8 ? k_piece : (uint32_t)((lane % PPR) ^ T::swz_v(wave * RPC + lane / PPR)) * 16;
   static_assert(NWAVES * RPC % 16 == 0, "a lane's chunks are alike");
   uint32_t koff[CPW], voff[CPW];
-  size_t k_at[CPW], v_at[CPW];                   // chunks' byte offsets in the pools
-  int kt = 0;                                    // the tile that k_at is of
+  uint32_t k_row[CPW], v_row[CPW];               // chunks' first slots in the pools
+  int kt = 0;                                    // the tile that k_row is of
   auto locate = [&]() __attribute__((always_inline)) {
     const int tok = seg0 + kt * KT;
     if (__builtin_expect((min(tok + KT - 1, last_tok) >> c.shift) - page0 - window >= 64, 0)) {
@@ -161,7 +166,7 @@ __global__ void __launch_bounds__(NWAVES * 64) __attribute__((amdgpu_waves_per_e
     for (int i = 0; i < CPW; i++) {
       const int t = min(tok + (i * NWAVES + wave_u) * RPC, last_chunk);
       const int number = __builtin_amdgcn_readlane(numbers, (t >> c.shift) - page0 - window);
-      k_at[i] = (size_t)((unsigned)(number << c.shift) + (unsigned)(t & mask)) * tok_bytes;
+      k_row[i] = (unsigned)(number << c.shift) + (unsigned)(t & mask);
     }
   };
   auto offsets_of_last = [&](uint32_t (&off)[CPW], uint32_t piece) {
@@ -173,7 +178,7 @@ __global__ void __launch_bounds__(NWAVES * 64) __attribute__((amdgpu_waves_per_e
   };
   auto next_tile = [&]() __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < CPW; i++) v_at[i] = k_at[i];
+    for (int i = 0; i < CPW; i++) v_row[i] = k_row[i];
     if (__builtin_expect(kt >= tl, 0)) offsets_of_last(voff, v_piece);
     // (a value that the compiler knows nothing of between the two: it joins their stores through a pointer, and both arrays go to memory)
     asm volatile("" : "+s"(kt));
@@ -184,7 +189,7 @@ __global__ void __launch_bounds__(NWAVES * 64) __attribute__((amdgpu_waves_per_e
     }
   };
   auto tload_chunk = [&](bool is_k, int slot, int i) {
-    dma(lds_0 + (uint32_t)((is_k ? 0 : 2 * TILE) + slot * TILE) * 2 + (uint32_t)(i * NWAVES + wave_u) * 1024, is_k ? k_base + k_at[i] : v_base + v_at[i],
+    dma(lds_0 + (uint32_t)((is_k ? 0 : 2 * TILE) + slot * TILE) * 2 + (uint32_t)(i * NWAVES + wave_u) * 1024, is_k ? k_base + (size_t)k_row[i] * tok_bytes : v_base + (size_t)v_row[i] * tok_bytes,
         is_k ? koff[i] : voff[i]);
   };
   auto tload = [&](bool is_k, int slot) {
@@ -194,7 +199,7 @@ __global__ void __launch_bounds__(NWAVES * 64) __attribute__((amdgpu_waves_per_e
   auto all_landed = [&]() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); };
   // FP8: eight codes a lane and chunk, in registers for a tile, then widened (exactly) into the same places
   struct Stage8 { uint2 r[CPW]; };
-  auto gload8_piece = [&](bool is_k, int i) { return *(const uint2*)((is_k ? k_base + k_at[i] : v_base + v_at[i]) + (is_k ? koff[i] : voff[i])); };
+  auto gload8_piece = [&](bool is_k, int i) { return *(const uint2*)((is_k ? k_base + (size_t)k_row[i] * tok_bytes : v_base + (size_t)v_row[i] * tok_bytes) + (is_k ? koff[i] : voff[i])); };
   auto gload8 = [&](bool is_k) {
     Stage8 st;
 #pragma unroll
@@ -261,7 +266,7 @@ __global__ void __launch_bounds__(NWAVES * 64) __attribute__((amdgpu_waves_per_e
   for (int i = 0; i < CPW; i++) {
     koff[i] = (uint32_t)(lane / PPR) * tok_bytes + k_piece;
     voff[i] = (uint32_t)(lane / PPR) * tok_bytes + v_piece;
-    k_at[i] = v_at[i] = 0;
+    k_row[i] = v_row[i] = 0;
   }
   Stage8 k8, v8, k8b;
   if (ntiles > 0) {
@@ -445,7 +450,9 @@ __global__ void __launch_bounds__(NWAVES * 64) __attribute__((amdgpu_waves_per_e
 
   // ---- normalised rows, or this segment's partials
   const float l_tot = l_run + __shfl_xor(l_run, 32, 64);
-  if (!c.part_o) {
+  const LateArgs late = late_args();
+  const size_t head_wg = ((size_t)bu * (unsigned)late->W + (unsigned)beam_wg) * (unsigned)late->Hq + kvh * (unsigned)late->g;
+  if (!late->part_o) {
     // The wave's 32 rows go through its own slice of LDS, so that memory sees whole rows
     uint16_t* s_o = smem + own_k;
     const float inv = l_tot > 0.f ? 1.0f / l_tot : 0.f;
@@ -461,24 +468,24 @@ __global__ void __launch_bounds__(NWAVES * 64) __attribute__((amdgpu_waves_per_e
         st.y = __builtin_bit_cast(uint32_t, hb);
         *(uint2*)(&s_o[n32 * D + ((4 * db + q4) ^ (n32 & (PPR - 1))) * 8 + 4 * G]) = st;
       }
-    uint16_t* out_b = c.out + head_wg * D;
+    uint16_t* out_b = late->out + head_wg * D;
 #pragma unroll
     for (int i = 0; i < 32 * PPR / 64; i++) {
       const int p = lane + 64 * i, rl = p / PPR, piece = p % PPR, rr = row_w + rl, beam = small_div(rr, c.rcp_g);
       const uint4 v = *(const uint4*)(&s_o[rl * D + (piece ^ (rl & (PPR - 1))) * 8]);
-      if (rr < M) *(uint4*)(out_b + (uint32_t)(((beam - beam_wg) * c.Hq + (rr - beam * c.g)) * D + piece * 8)) = v;
+      if (rr < M) *(uint4*)(out_b + (uint32_t)(((beam - beam_wg) * late->Hq + (rr - beam * late->g)) * D + piece * 8)) = v;
     }
-    if (c.lse && G == 0 && qrow >= 0)
-      c.lse[((size_t)bu * (unsigned)c.W + (unsigned)beam_q) * (unsigned)c.Hq + kvh * (unsigned)c.g + (unsigned)(qrow - beam_q * c.g)] =
+    if (late->lse && G == 0 && qrow >= 0)
+      late->lse[((size_t)bu * (unsigned)late->W + (unsigned)beam_q) * (unsigned)late->Hq + kvh * (unsigned)late->g + (unsigned)(qrow - beam_q * late->g)] =
           l_tot > 0.f ? (m_run + __builtin_amdgcn_logf(l_tot)) * kLn2 : -INFINITY;
   } else {
     // unnormalised O and (maximum, sum) as the lanes hold them: every store is a run of whole lines
     const int left = min(32, M - row_w);
-    const size_t unit = shared ? (size_t)(unsigned)sp * (unsigned)c.Hkv + kvh
-                               : (size_t)(unsigned)c.part0.ns * (unsigned)c.Hkv * (unsigned)c.B + ((size_t)bu * (unsigned)ns + (unsigned)sp) * (unsigned)c.Hkv + kvh;
+    const size_t unit = SHARED ? (size_t)(unsigned)sp * (unsigned)late->Hkv + kvh
+                               : (size_t)(unsigned)late->part0.ns * (unsigned)late->Hkv * (unsigned)late->B + ((size_t)bu * (unsigned)ns + (unsigned)sp) * (unsigned)late->Hkv + kvh;
     const size_t row_p = unit * (unsigned)M + (unsigned)row_w;
     if (qrow >= 0) {
-      f32x4* part = (f32x4*)(c.part_o + row_p * D) + G * left + n32;
+      f32x4* part = (f32x4*)(late->part_o + row_p * D) + G * left + n32;
 #pragma unroll
       for (int e = 0; e < D / 8; e++) {
         const f32x4 v = {o_acc[e / 4][0][4 * (e % 4)], o_acc[e / 4][0][4 * (e % 4) + 1], o_acc[e / 4][0][4 * (e % 4) + 2], o_acc[e / 4][0][4 * (e % 4) + 3]};
@@ -486,10 +493,292 @@ __global__ void __launch_bounds__(NWAVES * 64) __attribute__((amdgpu_waves_per_e
       }
       if (G == 0) {
         const f32x2 ml = {l_tot > 0.f ? m_run : -INFINITY, l_tot};
-        *(f32x2*)(c.part_ml + (row_p + n32) * 2) = ml;
+        *(f32x2*)(late->part_ml + (row_p + n32) * 2) = ml;
       }
     }
   }
+}
+
+// Up to 32 rows of a (request, KV head) pair: 32 rows of a workgroup of 128 would be all there is, and what counts is how soon the keys arrive.  Every wavefront
+// holds the rows and takes every fourth 32 tokens of the segment through places of its own in LDS: K's next 32 are asked for as soon as the scores
+// are made, V's as soon as its products are, and nobody waits for anybody until the four (maximum, sum, O) are joined in LDS.  The beams' own tokens are the
+// list's last tiles.  Bound: memory; two workgroups of four wavefronts to a CU have up to 128 KB of loads on their way.
+constexpr int paged_few_lds_bytes(int d) { return (4 * 2 * 32 + 32) * d * 2; }      // a K and a V place per wavefront, and Q
+constexpr int paged_mix_lds_bytes(int d) { return paged_lds_bytes(d, 128) > paged_few_lds_bytes(d) ? paged_lds_bytes(d, 128) : paged_few_lds_bytes(d); }
+
+template <int D, bool KV8>
+__device__ __forceinline__ void few_rows(const PagedCtx& c, const unsigned id) {
+  using T = AttnTile<D, 1>;
+  constexpr int PPR = D / 8, RPC = 1024 / (D * 2), FT = 32, PLACE = FT * D, NLD = FT / RPC;      // NLD: loads of a place
+  constexpr int EB = KV8 ? 1 : 2;
+  extern __shared__ __attribute__((aligned(1024))) uint16_t smem[];
+  const int tid = (int)threadIdx.x, wave = tid >> 6, lane = tid & 63, G = lane >> 5, n32 = lane & 31;
+  const int wave_u = __builtin_amdgcn_readfirstlane(wave);
+  const unsigned place = id >> 3, nth = div_by(place, (unsigned)c.part1.MB, c.part1.inv_mb);
+  const int group = (int)(nth * 8 + (id & 7u)), mbi = (int)(place - nth * (unsigned)c.part1.MB), ns = c.part1.ns, M = c.part1.M;
+  if (group >= c.part1.groups) return;
+  const unsigned gq = div_by((unsigned)group, (unsigned)ns, c.part1.inv_ns);
+  const int sp = group - (int)gq * ns;
+  const unsigned bu = div_by(gq, (unsigned)c.Hkv, c.inv_hkv), kvh = gq - bu * (unsigned)c.Hkv;
+  auto dma = [&](uint32_t lds_addr, const char* gbase, uint32_t off) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_addr), "v"(off), "s"(gbase) : "memory", "m0");
+  };
+  const uint32_t lds_0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint16_t*)smem;
+
+  // ---- Q, in one place for all
+  const int row_w = mbi * 32, beam0 = __builtin_amdgcn_readfirstlane(small_div(row_w, c.rcp_g));
+  const char* q_b = (const char*)scalar(c.q + (((size_t)bu * (unsigned)c.W + (unsigned)beam0) * (unsigned)c.Hq + kvh * (unsigned)c.g) * D);
+  constexpr int q_place = 8 * PLACE;
+  const int k_place = wave_u * 2 * PLACE, v_place = k_place + PLACE;
+#pragma unroll
+  for (int i = 0; i < NLD / 4; i++) {
+    const int ch = i * 4 + wave_u, rl = ch * RPC + lane / PPR, r = min(row_w + rl, M - 1), beam = small_div(r, c.rcp_g);
+    dma(lds_0 + (uint32_t)(q_place + ch * RPC * D) * 2, q_b,
+        (uint32_t)((beam - beam0) * c.Hq + (r - beam * c.g)) * (D * 2) + (uint32_t)(((lane % PPR) ^ T::swz_k(rl)) * 16));
+  }
+
+  const int L = __builtin_amdgcn_readfirstlane(c.max_L == 0 ? 0 : min(max(c.lens[bu], 0), c.max_L));
+  const int front = c.own_prefix, keys = front + L;
+  int chunk = (int)div_by((unsigned)keys + (unsigned)ns - 1u, (unsigned)ns, c.part1.inv_ns);
+  chunk = (chunk + KT - 1) / KT * KT;
+  const int seg0 = min(keys, sp * chunk), seg1 = min(keys, seg0 + chunk);
+  const int nt = (seg1 - seg0 + FT - 1) / FT;
+  const bool own_stage = c.u > 0 && sp == (max(0, keys - (ns - 1) * chunk) < chunk ? ns - 1 : 0);
+  const int qrow = row_w + n32 < M ? row_w + n32 : -1;
+  const int beam_q = small_div(max(qrow, 0), c.rcp_g);
+  const int Ru = own_stage ? (__builtin_amdgcn_readfirstlane(small_div(min(row_w + 31, M - 1), c.rcp_g)) - beam0 + 1) * c.u : 0;
+  const int my_lo = (beam_q - beam0) * c.u;
+  const int total = nt + (Ru + FT - 1) / FT;
+
+  // ---- page numbers: lane i has that of page window + i of the list
+  const int mask = (1 << c.shift) - 1, last_tok = seg1 - 1, last_chunk = last_tok & ~(RPC - 1), last_page = last_tok >> c.shift;
+  auto numbers_from = [&](int first) {
+    const int p = min(first + lane, max(last_page, 0)), q = p - (front >> c.shift);
+    int number = 0;
+    if (nt > 0) number = q < 0 ? c.prefix_pages[p] : c.table[(size_t)bu * (unsigned)c.max_pages + (unsigned)q];
+    return (unsigned)number < (unsigned)c.n_pages ? number : 0;
+  };
+  int window = seg0 >> c.shift, numbers = numbers_from(window);
+  const uint32_t tok_bytes = (uint32_t)c.Hkv * D * EB, own_bytes = (uint32_t)c.Hkv * D * 2;
+  const char* k_base = c.kp + (size_t)kvh * D * EB;
+  const char* v_base = c.vp + (size_t)kvh * D * EB;
+  const char* ku_b = (const char*)(c.ku + ((size_t)bu * (unsigned)(c.W * c.ND) * (unsigned)c.Hkv + kvh) * D);
+  const char* vu_b = (const char*)(c.vu + ((size_t)bu * (unsigned)(c.W * c.ND) * (unsigned)c.Hkv + kvh) * D);
+  // byte offset of a chunk of tile j in its pool, and of this lane's row in the chunk (rows behind the segment: its last token)
+  auto chunk_at = [&](int j, int i, uint32_t* lane_row) {
+    const int tok = seg0 + j * FT + i * RPC, t = min(tok, last_chunk), p = t >> c.shift;
+    if (p - window >= 64) { window = (seg0 + j * FT) >> c.shift; numbers = numbers_from(window); }      // (wave-uniform; a tile lies in four pages at most)
+    const int number = __builtin_amdgcn_readlane(numbers, p - window);
+    *lane_row = (uint32_t)(min(tok + lane / PPR, last_tok) - t) * tok_bytes;
+    return (size_t)((unsigned)(number << c.shift) + (unsigned)(t & mask)) * tok_bytes;
+  };
+  uint32_t own_off = 0;                          // byte offset in the request's own-token block of row lane % 32 of a tile of own tokens
+  auto own_rows = [&](int j) {
+    const int rho = (j - nt) * FT + n32;
+    int bl, tok;
+    divmod_small(rho < Ru ? rho : 0, c.u, c.rcp_u, &bl, &tok);
+    int prow = (beam0 + bl) * c.ND + tok;
+    if (c.slot) {                                // (an entry outside the block falls back to the beam's own row)
+      const int sl = c.slot[(size_t)bu * (unsigned)(c.W * c.ND) + (unsigned)prow];
+      prow = (unsigned)sl < (unsigned)(c.W * c.ND) ? sl : prow;
+    }
+    own_off = (uint32_t)prow * own_bytes;
+  };
+  struct Stage8 { uint2 r[KV8 ? NLD : 1]; };
+  Stage8 k8, v8;
+  auto ask = [&](bool is_k, int j) __attribute__((always_inline)) {
+    if (j < nt) {
+#pragma unroll
+      for (int i = 0; i < NLD; i++) {
+        uint32_t row;
+        const size_t at = chunk_at(j, i, &row);
+        const int r = i * RPC + lane / PPR;
+        if (KV8) (is_k ? k8 : v8).r[i] = *(const uint2*)((is_k ? k_base : v_base) + at + row + (uint32_t)(lane % PPR) * 8);
+        else dma(lds_0 + (uint32_t)((is_k ? k_place : v_place) * 2 + i * 1024), (is_k ? k_base : v_base) + at, row + (uint32_t)(((lane % PPR) ^ (is_k ? T::swz_k(r) : T::swz_v(r))) * 16));
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < NLD; i++) {
+        const int r = i * RPC + lane / PPR, piece = (lane % PPR) ^ (is_k ? T::swz_k(r) : T::swz_v(r));
+        dma(lds_0 + (uint32_t)((is_k ? k_place : v_place) * 2 + i * 1024), is_k ? ku_b : vu_b, (uint32_t)__shfl((int)own_off, r, 64) + (uint32_t)piece * 16);
+      }
+    }
+  };
+  // the tile is in its place: `later`: a tile's loads of the other kind came behind it
+  auto there = [&](bool is_k, int j, bool later) __attribute__((always_inline)) {
+    if (KV8 && j < nt) {
+#pragma unroll
+      for (int i = 0; i < NLD; i++) {
+        const uint2 w = (is_k ? k8 : v8).r[i];
+        const int r = i * RPC + lane / PPR;
+        const bf16x2 e01 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w.x, 1.0f, false), e23 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w.x, 1.0f, true);
+        const bf16x2 e45 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w.y, 1.0f, false), e67 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w.y, 1.0f, true);
+        uint4 x;
+        x.x = __builtin_bit_cast(uint32_t, e01); x.y = __builtin_bit_cast(uint32_t, e23);
+        x.z = __builtin_bit_cast(uint32_t, e45); x.w = __builtin_bit_cast(uint32_t, e67);
+        *(uint4*)(smem + (is_k ? k_place : v_place) + r * D + ((lane % PPR) ^ (is_k ? T::swz_k(r) : T::swz_v(r))) * 8) = x;
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    } else if (!KV8 && later) {
+      asm volatile("s_waitcnt vmcnt(%0)" ::"i"(NLD) : "memory");
+    } else {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    }
+  };
+
+  f32x16 o_acc[D / 32];
+#pragma unroll
+  for (int db = 0; db < D / 32; db++)
+#pragma unroll
+    for (int i = 0; i < 16; i++) o_acc[db][i] = 0.f;
+  float m_run = -INFINITY, l_run = 0.f;
+  const float cp = KV8 ? c.c * c.k_scale : c.c;
+  const typename T::Rd rdo = T::make_rd(lane, (int)lds_0);
+  int j = wave_u;
+  if (j < total) {
+    if (j >= nt) own_rows(j);
+    ask(true, j);
+    ask(false, j);
+    asm volatile("s_waitcnt vmcnt(%0)" ::"i"(2 * NLD) : "memory");           // (Q came before them)
+  } else {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  }
+  __syncthreads();
+  bf16x8 qop[D / 16];
+#pragma unroll
+  for (int ks = 0; ks < D / 16; ks++) qop[ks] = T::read_k(q_place, rdo, 0, ks);
+  bool own_units = !KV8;                         // O is in true units, not in those of the FP8 codes
+  for (; j < total; j += 4) {
+    const bool own = j >= nt, more = j + 4 < total;
+    there(true, j, true);
+    f32x16 s;
+#pragma unroll
+    for (int i = 0; i < 16; i++) s[i] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ks++) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(T::read_k(k_place, rdo, 0, ks), qop[ks], s, 0, 0, 0);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");                       // (K has been read)
+    if (more) {
+      if (j + 4 >= nt) own_rows(j + 4);
+      ask(true, j + 4);
+    }
+    // what the column may see of the tile: rows [lo, lo + n)
+    const int lo = own ? my_lo - (j - nt) * FT : 0;
+    const unsigned n = own ? (qrow >= 0 ? (unsigned)c.u : 0u) : (unsigned)(seg1 - (seg0 + j * FT));
+    const float cs = own ? c.c : cp;
+    float mx = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 16; i++) {
+      s[i] = (unsigned)(8 * (i / 4) + 4 * G + (i % 4) - lo) < n ? s[i] : -INFINITY;
+      mx = fmaxf(mx, s[i]);
+    }
+    mx = halves_max(mx) * cs;
+    if (KV8 && own && !own_units) {
+      own_units = true;
+#pragma unroll
+      for (int db = 0; db < D / 32; db++)
+#pragma unroll
+        for (int i = 0; i < 16; i++) o_acc[db][i] *= c.v_scale;
+    }
+    if (__any(mx > m_run)) {
+      const float m_new = fmaxf(m_run, mx), scale = mx > m_run ? __builtin_amdgcn_exp2f(m_run - m_new) : 1.f;
+      l_run *= scale;
+      m_run = m_new;
+#pragma unroll
+      for (int db = 0; db < D / 32; db++)
+#pragma unroll
+        for (int i = 0; i < 16; i++) o_acc[db][i] *= scale;
+    }
+    const float ref = m_run > -INFINITY ? m_run : 0.f;
+    float p[16];
+#pragma unroll
+    for (int i = 0; i < 16; i++) {
+      p[i] = __builtin_amdgcn_exp2f(fmaf(s[i], cs, -ref));
+      l_run += p[i];
+    }
+    bf16x8 pop[2];
+#pragma unroll
+    for (int t = 0; t < 2; t++)
+#pragma unroll
+      for (int e = 0; e < 8; e++) pop[t][e] = (__bf16)p[8 * t + e];
+    there(false, j, more);
+#pragma unroll
+    for (int t = 0; t < 2; t++)
+#pragma unroll
+      for (int db = 0; db < D / 32; db++) o_acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(T::read_v(v_place, rdo, t, db), pop[t], o_acc[db], 0, 0, 0);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");                       // (V has been read)
+    if (more) ask(false, j + 4);
+  }
+  if (!own_units) {
+#pragma unroll
+    for (int db = 0; db < D / 32; db++)
+#pragma unroll
+      for (int i = 0; i < 16; i++) o_acc[db][i] *= c.v_scale;
+  }
+
+  // ---- the four wavefronts' parts join in LDS, each in its own places; then every one has columns of its own to write
+  const float l_tot = l_run + __shfl_xor(l_run, 32, 64);
+  f32x2* s_ml = (f32x2*)(smem + q_place);        // (everybody had read Q when it first asked for K again; with one tile or none: at the barrier above)
+  f32x4* mine = (f32x4*)(smem + k_place) + lane;
+#pragma unroll
+  for (int e = 0; e < D / 8; e++) mine[64 * e] = f32x4{o_acc[e / 4][4 * (e % 4)], o_acc[e / 4][4 * (e % 4) + 1], o_acc[e / 4][4 * (e % 4) + 2], o_acc[e / 4][4 * (e % 4) + 3]};
+  __syncthreads();
+  if (G == 0) s_ml[wave * 32 + n32] = f32x2{l_tot > 0.f ? m_run : -INFINITY, l_tot};
+  __syncthreads();
+  if (qrow < 0) return;
+  float top = -INFINITY, l = 0.f, a[4];
+#pragma unroll
+  for (int w = 0; w < 4; w++) top = fmaxf(top, s_ml[w * 32 + n32].x);
+#pragma unroll
+  for (int w = 0; w < 4; w++) {
+    const f32x2 ml = s_ml[w * 32 + n32];
+    a[w] = ml.x > -INFINITY ? __builtin_amdgcn_exp2f(ml.x - top) : 0.f;
+    l += ml.y * a[w];
+  }
+  const LateArgs late = late_args();
+  const float inv = late->part_o ? 1.f : l > 0.f ? 1.0f / l : 0.f;
+  const size_t row = ((size_t)bu * (unsigned)late->W + (unsigned)beam_q) * (unsigned)late->Hq + kvh * (unsigned)late->g + (unsigned)(qrow - beam_q * late->g);
+  const int left = min(32, M - row_w);
+  const size_t row_p = ((size_t)(unsigned)late->part0.ns * (unsigned)late->Hkv * (unsigned)late->B + ((size_t)bu * (unsigned)ns + (unsigned)sp) * (unsigned)late->Hkv + kvh) * (unsigned)M + (unsigned)row_w;
+  f32x4* part = (f32x4*)(late->part_o + row_p * D) + G * left + n32;
+  constexpr int EW = D / 32;                     // pieces of four columns (8 e + 4 G ..) of a row that a wavefront has
+#pragma unroll
+  for (int k = 0; k < EW; k++) {
+    const int e = wave_u * EW + k;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < 4; w++) {
+      const f32x4 x = *((const f32x4*)(smem + w * 2 * PLACE) + 64 * e + lane);
+#pragma unroll
+      for (int i = 0; i < 4; i++) o[i] += x[i] * a[w];
+    }
+    if (late->part_o) {
+      part[2 * e * left] = o;
+    } else {
+      bf16x4 h;
+#pragma unroll
+      for (int i = 0; i < 4; i++) h[i] = (__bf16)(o[i] * inv);
+      *(bf16x4*)(late->out + row * D + 8 * e + 4 * G) = h;
+    }
+  }
+  if (wave == 0 && G == 0) {
+    if (late->part_o) *(f32x2*)(late->part_ml + (row_p + n32) * 2) = f32x2{top, l};
+    else if (late->lse) late->lse[row] = l > 0.f ? (top + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+  }
+}
+
+// All rows by blocks of 128 or 256; all by blocks of 32; the prefix by blocks of 128 of all requests' rows, which are dealt first, and each request's list by blocks of 32.
+template <int D, int NWAVES, bool KV8>
+__global__ void __launch_bounds__(NWAVES * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) k_paged_attn(PagedCtx c) {
+  tile_rows<D, NWAVES, KV8, false>(c, blockIdx.x);
+}
+template <int D, bool KV8>
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, D == 64 ? 4 : 2))) k_paged_few(PagedCtx c) {
+  few_rows<D, KV8>(c, blockIdx.x);
+}
+template <int D, bool KV8>
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) k_paged_mix(PagedCtx c) {
+  if (blockIdx.x < c.grid0) tile_rows<D, 4, KV8, true>(c, blockIdx.x);
+  else few_rows<D, KV8>(c, blockIdx.x - c.grid0);
 }
 
 // Joins a row's partials: those of part 0, whose rows are all requests' in one, then those of part 1.  A lane takes four columns of a row; eight rows of eight
@@ -555,8 +844,8 @@ __global__ void __launch_bounds__(256) k_paged_join(PagedCtx c) {
   if (c.lse && piece == 0) c.lse[row] = L > 0.f ? (M2 + __builtin_amdgcn_logf(L)) * kLn2 : -INFINITY;
 }
 
-// The launch: rows of a workgroup, whether the prefix is met by all requests' rows together (ns[0] > 0), and segments of the keys.
-struct PagedPlan { int mwg, ns[2]; };
+// The launch: rows of a workgroup of part 1 (32, 128, 256), whether the prefix is met by all requests' rows together (ns[0] > 0; then 32), and segments of the keys.
+struct PagedPlan { int rows, ns[2]; };
 PagedPlan plan_paged(const gr_attn_paged_params* p) {
   PagedPlan plan;
   const int64_t g = p->Hq / p->Hkv, M = p->W * g, all = p->B * M;
@@ -564,16 +853,16 @@ PagedPlan plan_paged(const gr_attn_paged_params* p) {
   // packed, the prefix is met by so many blocks of 128 rows instead of so many
   const bool pack = p->prefix_L > 0 && p->B > 1 && all < ((int64_t)1 << 22) && blocks(all, 128) * 2 <= p->B * blocks(M, 128);
   const int64_t units256 = (int64_t)p->B * p->Hkv * blocks(M, 256);
-  plan.mwg = !pack && M > 128 && units256 >= 256 ? 256 : 128;
-  // segments for about two workgroups per CU, none under four tiles; and no more pages in one than have room
-  auto segments = [&](int64_t units, int64_t tokens) {
-    const int64_t most = tokens / (4 * KT), want = (512 + units / 2) / units, room = (tokens + (int64_t)kSegPages * p->page_size - 1) / ((int64_t)kSegPages * p->page_size);
+  plan.rows = pack || M <= 32 ? 32 : M > 128 && units256 >= 256 ? 256 : 128;
+  // segments for about `wanted` workgroups, none under `least` tokens; and no more pages in one than have room
+  auto segments = [&](int64_t wanted, int64_t units, int64_t tokens, int64_t least) {
+    const int64_t most = tokens / least, want = (wanted + units / 2) / units, room = (tokens + (int64_t)kSegPages * p->page_size - 1) / ((int64_t)kSegPages * p->page_size);
     int64_t n = want < most ? want : most;
     n = n < 1 ? 1 : n > 16 ? 16 : n;
     return (int)(n < room ? room : n);
   };
-  plan.ns[0] = pack ? segments(p->Hkv * blocks(all, plan.mwg), p->prefix_L) : 0;
-  plan.ns[1] = segments((int64_t)p->B * p->Hkv * blocks(M, plan.mwg), (pack ? 0 : (int64_t)p->prefix_L) + p->max_L);
+  plan.ns[0] = pack ? segments(256, p->Hkv * blocks(all, 128), p->prefix_L, 4 * KT) : 0;
+  plan.ns[1] = segments(512, (int64_t)p->B * p->Hkv * blocks(M, plan.rows), (pack ? 0 : (int64_t)p->prefix_L) + p->max_L, 4 * KT);
   return plan;
 }
 
@@ -633,7 +922,7 @@ extern "C" gr_status gr_beam_attn_paged(const gr_attn_paged_params* p, void* wor
   int64_t grid = 0;
   for (int k = 0; k < 2; k++) {
     const int64_t M = k == 0 ? p->B * p->W * g : p->W * g, pairs = (k == 0 ? 1 : (int64_t)p->B) * p->Hkv;
-    const int64_t MB = (M + plan.mwg - 1) / plan.mwg, groups = pairs * plan.ns[k], wgs = (groups + 7) / 8 * 8 * MB;
+    const int64_t rows = k == 0 ? 128 : plan.rows, MB = (M + rows - 1) / rows, groups = pairs * plan.ns[k], wgs = (groups + 7) / 8 * 8 * MB;
     if (groups >= ((int64_t)1 << 31) || grid + wgs >= ((int64_t)1 << 31)) return GR_ERR_UNSUPPORTED;
     if (k == 0) c.grid0 = (unsigned)wgs;
     grid += wgs;
@@ -648,16 +937,22 @@ extern "C" gr_status gr_beam_attn_paged(const gr_attn_paged_params* p, void* wor
     c.part_o = (float*)workspace;
     c.part_ml = (float*)((char*)workspace + gr_align256(rows * p->d * 4));
   }
-  const size_t lds = paged_lds_bytes(p->d, plan.mwg);
-#define GR_LAUNCH(...)                                                                                                     \
+#define GR_LAUNCH(LDS, THREADS, ...)                                                                                       \
   do {                                                                                                                     \
-    if (const gr_status st = gr_allow_lds<k_paged_attn<__VA_ARGS__>>(lds)) return st;                                      \
-    hipLaunchKernelGGL((k_paged_attn<__VA_ARGS__>), dim3((unsigned)grid), dim3(2 * plan.mwg), lds, stream, c);             \
+    const size_t lds = LDS;                                                                                                \
+    if (const gr_status st = gr_allow_lds<__VA_ARGS__>(lds)) return st;                                                    \
+    hipLaunchKernelGGL((__VA_ARGS__), dim3((unsigned)grid), dim3(THREADS), lds, stream, c);                                \
   } while (0)
-#define GR_LAUNCH_TYPES(DD, NW) do { if (kv8) GR_LAUNCH(DD, NW, true); else GR_LAUNCH(DD, NW, false); } while (0)
-  if (p->d == 128) { if (plan.mwg == 256) GR_LAUNCH_TYPES(128, 8); else GR_LAUNCH_TYPES(128, 4); }
-  else { if (plan.mwg == 256) GR_LAUNCH_TYPES(64, 8); else GR_LAUNCH_TYPES(64, 4); }
-#undef GR_LAUNCH_TYPES
+#define GR_LAUNCH_ROWS(DD, K8)                                                                                             \
+  do {                                                                                                                     \
+    if (plan.ns[0]) GR_LAUNCH(paged_mix_lds_bytes(DD), 256, k_paged_mix<DD, K8>);                                          \
+    else if (plan.rows == 32) GR_LAUNCH(paged_few_lds_bytes(DD), 256, k_paged_few<DD, K8>);                                \
+    else if (plan.rows == 128) GR_LAUNCH(paged_lds_bytes(DD, 128), 256, k_paged_attn<DD, 4, K8>);                          \
+    else GR_LAUNCH(paged_lds_bytes(DD, 256), 512, k_paged_attn<DD, 8, K8>);                                                \
+  } while (0)
+  if (p->d == 128) { if (kv8) GR_LAUNCH_ROWS(128, true); else GR_LAUNCH_ROWS(128, false); }
+  else { if (kv8) GR_LAUNCH_ROWS(64, true); else GR_LAUNCH_ROWS(64, false); }
+#undef GR_LAUNCH_ROWS
 #undef GR_LAUNCH
   if (c.part_o) {
     const int rpw = 1024 / p->d;
