@@ -135,7 +135,7 @@ struct WriteCtx {
   uint32_t rows_wg;                    // rows of a workgroup
   uint32_t n_slots;
   int64_t k_stride, v_stride;          // elements between rows of the inputs
-  float k_scale, v_scale;
+  float k_scale, v_scale, k_rcp, v_rcp;
   const uint16_t* k;
   const uint16_t* v;
   const int32_t* slot;
@@ -147,12 +147,24 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 // Eight bf16 values as E4M3 codes of x / scale: the division in fp32 as IEEE has it, saturated, rounded to nearest even; NaN stays NaN.
-__device__ __forceinline__ u32x2 codes8(u32x4 w, float scale) {
+// FAST: the quotient from the scale's reciprocal r (rounded to nearest) and one correction by the exact remainder, q = q0 + (x - q0 scale) r with q0 = x r, which rounds as the
+// division does (Markstein's theorem; compared with it on all finite bf16 values over 3000 scales from 2^-60 to 2^60, outside of which the remainder may underflow).
+// q0 is held within +-512, so that an infinite one does not make the remainder NaN: the result saturates all the same.  16 x 60-700 rows of 8 x 128 from a fused projection
+// 10.0 us with the division.
+template <bool FAST>
+__device__ __forceinline__ u32x2 codes8(u32x4 w, float scale, float r) {
   float f[8];
 #pragma unroll
   for (int i = 0; i < 8; i++) {
-    const float y = __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16) / scale;
-    f[i] = y != y ? y : fminf(fmaxf(y, -448.f), 448.f);
+    const float x = __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+    float y;
+    if (FAST) {
+      const float q0 = fminf(fmaxf(x * r, -512.f), 512.f);
+      y = copysignf(fmaf(fmaf(-q0, scale, x), r, q0), x);        // (-0 lost its sign)
+    } else {
+      y = x / scale;
+    }
+    f[i] = x != x ? x : fminf(fmaxf(y, -448.f), 448.f);
   }
   int a = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], 0, false);
   a = __builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], a, true);
@@ -163,7 +175,7 @@ __device__ __forceinline__ u32x2 codes8(u32x4 w, float scale) {
 
 // Bound: memory, 4 bytes an element in and out (FP8: 3).  A thread moves U pieces of 16 bytes of K and of V; all its rows are on their way before the
 // slots are needed.
-template <bool FP8, int U>
+template <int FP8, int U>      // FP8: 0 bf16, 1 codes by the corrected reciprocal, 2 by the division
 __global__ void __launch_bounds__(256) k_page_write(WriteCtx c) {
   const uint32_t row0 = blockIdx.x * c.rows_wg, n = min(c.rows_wg, c.T - row0) * c.pieces;
   for (uint32_t i0 = threadIdx.x; i0 < n; i0 += 256 * U) {
@@ -184,8 +196,8 @@ __global__ void __launch_bounds__(256) k_page_write(WriteCtx c) {
       if ((uint32_t)to[u] >= c.n_slots) continue;
       const size_t at = (size_t)(uint32_t)to[u] * c.pieces + piece[u];
       if (FP8) {
-        ((u32x2*)c.k_pages)[at] = codes8(kx[u], c.k_scale);
-        ((u32x2*)c.v_pages)[at] = codes8(vx[u], c.v_scale);
+        ((u32x2*)c.k_pages)[at] = codes8<FP8 == 1>(kx[u], c.k_scale, c.k_rcp);
+        ((u32x2*)c.v_pages)[at] = codes8<FP8 == 1>(vx[u], c.v_scale, c.v_rcp);
       } else {
         ((u32x4*)c.k_pages)[at] = kx[u];
         ((u32x4*)c.v_pages)[at] = vx[u];
@@ -241,15 +253,17 @@ extern "C" gr_status gr_page_write(const gr_page_write_params* p, void* stream_)
   WriteCtx c;
   c.T = (uint32_t)p->T; c.pieces = (uint32_t)(n / 8); c.inv_pieces = 0xffffffffu / c.pieces;
   c.n_slots = (uint32_t)(p->n_pages * p->page_size);
-  c.k_stride = p->k_stride; c.v_stride = p->v_stride; c.k_scale = p->k_scale; c.v_scale = p->v_scale;
+  c.k_stride = p->k_stride; c.v_stride = p->v_stride; c.k_scale = p->k_scale; c.v_scale = p->v_scale; c.k_rcp = 1.0f / p->k_scale; c.v_rcp = 1.0f / p->v_scale;
   c.k = (const uint16_t*)p->k; c.v = (const uint16_t*)p->v; c.slot = p->slot; c.k_pages = p->k_pages; c.v_pages = p->v_pages;
   const int64_t all = (int64_t)c.T * c.pieces;
   const int u = all >= (int64_t)256 * 4 * 512 ? 4 : 1;
   c.rows_wg = (uint32_t)((256 * u + c.pieces - 1) / c.pieces);
   const unsigned grid = (c.T + c.rows_wg - 1) / c.rows_wg;
 #define GR_LAUNCH(F, U_) hipLaunchKernelGGL((k_page_write<F, U_>), dim3(grid), dim3(256), 0, stream, c)
-  if (u == 4) { if (fp8) GR_LAUNCH(true, 4); else GR_LAUNCH(false, 4); }
-  else { if (fp8) GR_LAUNCH(true, 1); else GR_LAUNCH(false, 1); }
+  auto ordinary = [](float s) { return s >= 0x1p-60f && s <= 0x1p60f; };
+  const int type = !fp8 ? 0 : ordinary(p->k_scale) && ordinary(p->v_scale) ? 1 : 2;
+  if (u == 4) { if (type == 0) GR_LAUNCH(0, 4); else if (type == 1) GR_LAUNCH(1, 4); else GR_LAUNCH(2, 4); }
+  else { if (type == 0) GR_LAUNCH(0, 1); else if (type == 1) GR_LAUNCH(1, 1); else GR_LAUNCH(2, 1); }
 #undef GR_LAUNCH
   GR_HIP_TRY(hipGetLastError());
   return GR_OK;

@@ -381,35 +381,76 @@ __global__ void __launch_bounds__(256) k_paged_join(JoinCtx c) {
 
 // The launch.  rows: of a workgroup of part 1 (32, 128, 256); ns: segments of the prefix in part 0 (0: there is none) and of the list in part 1; ks and find as in gr_beam_attn.
 struct PagedPlan { int rows, ns[2], ks; bool find; };
+
+// More than 80 rows of a (request, KV head) pair are launched as gr_beam_attn launches them.  For fewer, the cheapest of these is taken, by their estimated time in us: blocks of 32 rows or of 128
+// over the whole list, or the prefix packed, each with 1 to 16 segments.  The estimate of a launch is `start`, and the longer of
+//   - what its keys take at `rate`;
+//   - its workgroups' time: `few` + `few_step` for every 128 tokens (blocks of 32), `unit` + `tile1` for every 64 (128; two sets of wavefronts where there is at most one workgroup per CU:
+//     `tile2` for every 128), `shared` + `shared_tile` for every 64 (part 0), times the rounds that an XCD's 32 CUs take them in (`few_per_cu` workgroups to a CU, two of part 0 and 1);
+// and, where there are several segments, `join` and the partials written and read at 3.1 TB/s.  Fitted to 870 random calls of 1 to 128 requests of 10 to 16384 tokens with 1 to 80 rows,
+// 430 of them behind a prefix of 64 to 8192 tokens, each timed in up to 40 ways: the mean call takes 1.04 times the best of them (packed wherever that saves half of the blocks,
+// with segments for about one or two workgroups per CU, 1.07 without a prefix and 1.14 with one), the worst 1.39.
+struct PagedCost { double start, few, few_step, few_per_cu, unit, tile1, tile2, shared, shared_tile, join, rate; };
+constexpr PagedCost kPagedCost[2][2] = {      // [head size 128][FP8]; rate in bytes a us
+    {{3.3, 1.5, 1.2, 2.0, 2.0, 1.05, 0.95, 1.5, 0.7, 3.1, 8.0e6}, {3.3, 1.5, 1.4, 2.0, 2.0, 1.05, 0.95, 1.5, 0.8, 3.1, 4.0e6}},
+    {{5.0, 0.5, 2.0, 1e4, 1.7, 1.1, 1.25, 0.5, 0.9, 2.5, 6.9e6}, {5.0, 0.5, 2.2, 1.5, 1.7, 1.4, 1.5, 0.5, 1.0, 2.5, 4.4e6}}};
+
 PagedPlan plan_paged(const gr_attn_paged_params* p) {
-  PagedPlan plan;
-  const int64_t g = p->Hq / p->Hkv, M = p->W * g, all = p->B * M;
-  auto blocks = [](int64_t rows, int of) { return (rows + of - 1) / of; };
-  auto segments = [&](int64_t wanted, int64_t units, int64_t tokens) {      // about `wanted` workgroups, none under four tiles
-    const int64_t most = tokens / (4 * KT), want = (wanted + units / 2) / units, n = want < most ? want : most;
-    return (int)(n < 1 ? 1 : n > 16 ? 16 : n);
-  };
-  // packed, the prefix is met by so many blocks of 128 rows instead of so many (offsets inside the packed rows fit 32 bits)
-  const bool pack = p->prefix_L > 0 && p->B > 1 && all < ((int64_t)1 << 22) && (int64_t)p->B * p->W * p->Hq * p->d < ((int64_t)1 << 31) &&
-                    blocks(all, 128) * 2 <= p->B * blocks(M, 128);
-  plan.ns[0] = pack ? segments(256, p->Hkv * blocks(all, 128), p->prefix_L) : 0;
-  plan.ks = 1; plan.find = false;
-  if (pack || M <= 32) {
-    plan.rows = 32;
-    plan.ns[1] = segments(512, (int64_t)p->B * p->Hkv * blocks(M, 32), (pack ? 0 : (int64_t)p->prefix_L) + p->max_L);
+  PagedPlan plan{};
+  const int64_t g = p->Hq / p->Hkv, M = p->W * g, all = p->B * M, pairs = (int64_t)p->B * p->Hkv;
+  const bool kv8 = p->kv_type == GR_KV_FP8;
+  auto parts = [](int64_t n, int64_t of) { return (n + of - 1) / of; };
+  if (M > 80) {
+    gr_attn_params q{};
+    q.B = p->B; q.W = p->W; q.Hq = p->Hq; q.Hkv = p->Hkv; q.d = p->d; q.max_L = p->prefix_L + p->max_L;
+    q.total_L = (int64_t)q.B * q.max_L;                      // (the lengths are on the GPU)
+    const AttnPlan a = plan_attn(&q, kv8);
+    plan.rows = a.mwg; plan.ns[1] = a.nsplit; plan.ks = a.ks;
+    plan.find = a.many && a.ks == 1 && p->B >= 2 && p->B <= kRankB;
     return plan;
   }
-  gr_attn_params q{};
-  q.B = p->B; q.W = p->W; q.Hq = p->Hq; q.Hkv = p->Hkv; q.d = p->d; q.max_L = p->prefix_L + p->max_L;
-  q.total_L = (int64_t)q.B * q.max_L;                        // (the lengths are on the GPU)
-  const AttnPlan a = plan_attn(&q, p->kv_type == GR_KV_FP8);
-  plan.rows = a.mwg; plan.ns[1] = a.nsplit; plan.ks = a.ks;
-  plan.find = a.many && a.ks == 1 && p->B >= 2 && p->B <= kRankB;
+  const PagedCost& c = kPagedCost[p->d == 128][kv8];
+  const double partial_us = 2.0 * p->B * p->W * p->Hq * p->d * 4 / 3.1e6, token_bytes = 2.0 * p->Hkv * p->d * (kv8 ? 1 : 2);
+  constexpr int kCounts[] = {1, 2, 3, 4, 6, 8, 12, 16};
+  double least = 0;
+  auto look_at = [&](int rows, int n0, int n1, int ks, double us) {
+    const int n = n0 + n1;
+    us += n > 1 ? c.join + partial_us * n : 0.0;
+    if (plan.rows && !(us < least)) return;
+    least = us;
+    plan.rows = rows; plan.ns[0] = n0; plan.ns[1] = n1; plan.ks = ks;
+  };
+  auto larger = [](double a, double b) { return a > b ? a : b; };
+  const int64_t list = (int64_t)p->prefix_L + p->max_L;
+  const double list_us = list * p->B * token_bytes / c.rate;
+  for (const int n : kCounts) {
+    if (n > 1 && n * 96 > list) break;
+    const double tiles = (double)parts(parts(list, n), KT);
+    const double few = (c.few + c.few_step * tiles / 2) * larger(1.0, parts(pairs * n, 8) * parts(M, 32) / (32 * c.few_per_cu));
+    look_at(32, 0, n, 1, larger(few, list_us));
+    const bool sets = list > KT && pairs * parts(M, 128) * n <= 256;
+    const int64_t on_xcd = parts(pairs * n, 8) * parts(M, 128);
+    const double unit = sets ? (c.unit + c.tile2 * (double)(((int64_t)tiles + 1) >> 1)) * (double)parts(on_xcd, 32) : (c.unit + c.tile1 * tiles) * larger(1.0, on_xcd / 64.0);
+    look_at(128, 0, n, sets ? 2 : 1, larger(unit, list_us));
+  }
+  // packed, as the beams of one request (offsets inside its rows fit 32 bits)
+  if (p->prefix_L > 0 && p->B > 1 && all < ((int64_t)1 << 22) && (int64_t)p->B * p->W * p->Hq * p->d < ((int64_t)1 << 31)) {
+    for (const int n0 : kCounts) {
+      if (n0 > 1 && n0 * 96 > p->prefix_L) break;
+      const double shared = c.shared + c.shared_tile * (double)parts(parts(p->prefix_L, n0), KT), shared_all = shared * (double)(parts((int64_t)p->Hkv * n0, 8) * parts(all, 128));
+      for (const int n1 : {1, 2, 4}) {
+        if (n1 > 1 && n1 * 128 > p->max_L) break;
+        const double few = c.few + c.few_step * (double)parts(parts(p->max_L, n1), KT) / 2;
+        look_at(32, n0, n1, 1, larger(larger(few, shared), (shared_all + few * (double)(parts(pairs * n1, 8) * parts(M, 32))) / 64));
+      }
+    }
+  }
+  plan.find = plan.rows == 128 && plan.ks == 1 && pairs * parts(M, 128) * plan.ns[1] > 256 && p->B >= 2 && p->B <= kRankB;
   return plan;
 }
 
 size_t paged_workspace(const gr_attn_paged_params* p, const PagedPlan& plan) {
-  const int n = plan.ns[0] + plan.ns[1];
+  const int n = plan.ns[0] + plan.ns[1];                     // (a packed prefix always joins: part 1 has the lists and the own tokens)
   if (n == 1) return 0;
   const size_t rows = (size_t)p->B * p->W * p->Hq * n;
   return gr_align256(rows * p->d * 4) + gr_align256(rows * 8);
