@@ -286,3 +286,22 @@ def test_graph_replays():
         torch.cuda.synchronize()
         assert torch.equal(out, got[0]) and torch.equal(lse, got[1])
         check(dict(s, lens=list(n)), got=got)
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("W,lens,P,d,page", [(128, [900, 333, 64], 0, 128, 16), (40, [1500, 700], 0, 64, 32), (300, [400] * 40, 0, 64, 16), (3, [700] * 20, 640, 128, 64),
+                                             (130, [300, 500], 256, 128, 16), (2, [600], 0, 64, 16)])
+def test_scores_that_rise_by_more_than_a_float_holds(W, lens, P, d, page, fp8):
+    """Quiet keys first; behind them a few keys whose scores are 100 and more powers of two higher, twice: sums against the first keys' maximum overflow."""
+    s = make(19, lens, W, 8, 2, d, page, P=P, u=2, fp8=fp8, width=6.0)
+    for b, n in enumerate(lens):
+        pages = torch.cat([s["prefix"], s["table"][b, :-(-n // page)]]).long()
+        t = torch.arange(P + n)
+        at = pages[t // page] * page + t % page
+        size = torch.full((P + n,), 0.06)
+        size[150 + b % 5:151 + b % 5] = 4.0            # inside a tile of 64
+        size[290:297] = 8.0
+        k = torch.randn((P + n, 2, d), generator=torch.Generator().manual_seed(P)) * size[:, None, None]      # (the prefix's keys are the same for all)
+        rows = s["k"].view(-1, 2, d)
+        rows[at] = (k / s["k_scale"]).clamp(-448, 448).to(torch.float8_e4m3fn).view(torch.uint8) if fp8 else k.bfloat16()
+    check(s)
