@@ -324,10 +324,10 @@ typedef struct {
 gr_status gr_page_map(const gr_page_map_params* p, void* stream);
 
 /* gr_page_write - row t of k and v (Hkv * d elements, rows k_stride and v_stride elements apart: they may be parts of a fused projection's rows) goes to slot
- * slot[t] of the pools.  Rows whose slot is outside [0, n_pages * page_size) are not written; which row is kept where two have the same slot is
- * not defined.  GR_KV_FP8: code = the E4M3 value nearest to x / scale (ties to even; the division is rounded to fp32 first), values beyond
- * +-448 saturate, NaN stays NaN.  Only enqueues on `stream`.  Supported: Hkv * d and the strides multiples of 8; T and n_pages * page_size
- * below 2^31.  k, v and the pools 16-byte aligned.  Errors: INVALID_ARG, UNSUPPORTED, HIP. */
+ * slot[t] of the pools.  Rows whose slot is outside [0, n_pages * page_size) are not written; a slot that two rows have holds either's
+ * elements, in parts too.  The pools do not overlap k, v or each other.  GR_KV_FP8: code = the E4M3 value nearest to x / scale (ties to even; the division is rounded to fp32 first), values beyond
+ * +-448 saturate, NaN stays NaN.  Only enqueues on `stream`.  Supported: Hkv * d (at most 2^20) and the strides multiples of 8; T and
+ * n_pages * page_size below 2^31.  k, v and the pools 16-byte aligned.  Errors: INVALID_ARG, UNSUPPORTED, HIP. */
 typedef struct {
   int64_t T;                      /* rows                                                              */
   int32_t Hkv, d, page_size, n_pages;
@@ -350,7 +350,7 @@ gr_status gr_page_write(const gr_page_write_params* p, void* stream);
  * What a table holds beyond a request's pages is not read; a page number outside [0, n_pages) is read as page 0, and a length outside [0, max_L] as the
  * nearer end.  Slots of a page behind a request's last token may hold anything.
  * GR_KV_FP8: pools of E4M3 codes, scales applied as in gr_beam_attn_fp8kv.
- * Supported: d in {64, 128}; Hq % Hkv == 0; 0 <= u <= ND; prefix_L a multiple of page_size; n_pages * page_size and prefix_L + max_L below 2^31;
+ * Supported: d in {64, 128}; Hq % Hkv == 0; 0 <= u <= ND; prefix_L a multiple of page_size; n_pages * page_size below 2^31; prefix_L + max_L below 2^30;
  * Hkv * d <= 65536; W * Hq/Hkv < 2^22.  bf16 tensors and pools 16-byte aligned; finite values in the slots that are read; |v| * 2^8 * (number of keys) below 2^128.
  * Workspace (device, 256-byte aligned, contents unspecified before and after): partial results of segments, where a row's keys are split.
  * Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE_TOO_SMALL, HIP. */
@@ -392,7 +392,7 @@ gr_status gr_beam_attn_paged(const gr_attn_paged_params* p, void* workspace, siz
  * in fp32.  Rows of dead beams are left as they are.  `out` is `logits` itself (in place; rows without a bias or a mask are then changed at the counted
  * tokens alone) or does not overlap it.  Any of the parts may be absent (NULL).  repetition is positive.  History rows whose
  * token lies outside [0, V) count nothing.
- * Supported: 1 <= V <= 32768; depth <= 8.  Only enqueues on `stream`.  Errors: INVALID_ARG, UNSUPPORTED, HIP.
+ * Supported: 1 <= V <= 32768; depth <= 8; n_history < 2^28.  Only enqueues on `stream`.  Errors: INVALID_ARG, UNSUPPORTED, HIP.
  * ------------------------------------------------------------------------------------------------ */
 typedef struct {
   int32_t B, W, V, depth, step;   /* 0 <= step < depth                                                 */

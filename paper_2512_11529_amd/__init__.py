@@ -385,7 +385,7 @@ def gr_page_write(k, v, slot, k_pages, v_pages, k_scale=1.0, v_scale=1.0, stream
 
 
 def attn_paged_workspace_bytes(B, W, Hq, Hkv, d, max_L, prefix_L=0, fp8=False, page_size=16) -> int:
-    """Workspace bytes of gr_beam_attn_paged.  Without page_size: enough for pages of any size."""
+    """Workspace bytes of gr_beam_attn_paged (the same for pages of any size)."""
     p = _AttnPagedParams()
     p.B, p.W, p.Hq, p.Hkv, p.d, p.max_L, p.prefix_L, p.kv_type, p.page_size = B, W, Hq, Hkv, d, int(max_L), int(prefix_L), int(bool(fp8)), int(page_size)
     return int(load_library().gr_beam_attn_paged_workspace_bytes(ctypes.byref(p)))

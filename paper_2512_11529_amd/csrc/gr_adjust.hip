@@ -18,6 +18,7 @@ constexpr int kTile = 8192;              // tokens of a workgroup, at most, of a
 constexpr int kSparseRows = 8;           // rows of a workgroup that streams none
 constexpr int kMaxV = 32768;
 constexpr int kMaxDepth = 8;
+constexpr int kMaxHistory = 1 << 28;     // (kSparseRows rows that all of them continue: the list's length is an int)
 constexpr int kFew = 256;                 // counted against each other
 constexpr int kList = 1024;
 constexpr int kBins = 4096;
@@ -280,7 +281,7 @@ extern "C" gr_status gr_logits_adjust(const gr_logits_adjust_params* p, void* st
        (uintptr_t)p->repetition | (uintptr_t)p->frequency | (uintptr_t)p->presence | (uintptr_t)p->bias | (uintptr_t)p->allowed |
        (uintptr_t)p->allowed_row) & 3)
     return GR_ERR_INVALID_ARG;
-  if (p->V > kMaxV || p->depth > kMaxDepth) return GR_ERR_UNSUPPORTED;
+  if (p->V > kMaxV || p->depth > kMaxDepth || p->n_history >= kMaxHistory) return GR_ERR_UNSUPPORTED;
   const int64_t rows = (int64_t)p->B * p->W;
   const uint64_t bytes = (uint64_t)rows * p->V * 4, from = (uint64_t)(uintptr_t)p->logits, to = (uint64_t)(uintptr_t)p->out;
   const bool inplace = from == to;

@@ -284,6 +284,13 @@ PyObject* slot_update(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// a number of the C ABI's structs
+int32_t int32_of(int64_t v, const char* name) {
+  if (v == (int32_t)v) return (int32_t)v;
+  PyErr_Format(PyExc_ValueError, "%s: %lld does not fit 32 bits", name, (long long)v);
+  throw Error();
+}
+
 // page_map(seq_lens, new_lens, free_pages, block_table, page_size, n_pages, total_new, lens, cu_new, slot, taken, stream) -> status
 PyObject* page_map(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded([&]() -> PyObject* {
@@ -298,8 +305,8 @@ PyObject* page_map(PyObject*, PyObject* const* a, Py_ssize_t n) {
     on.add("block_table", table);
     const int64_t B = table.size(0), free_pages = tensor_nd(a[2], at::kInt, "free_pages", 1).size(0);
     gr_page_map_params p{};
-    p.B = (int32_t)B; p.max_pages = (int32_t)table.size(1); p.page_size = (int32_t)integer(a[4]); p.n_pages = (int32_t)integer(a[5]);
-    p.n_free = (int32_t)free_pages; p.total_new = integer(a[6]);
+    p.B = (int32_t)B; p.max_pages = int32_of(table.size(1), "block_table"); p.page_size = int32_of(integer(a[4]), "page_size"); p.n_pages = int32_of(integer(a[5]), "n_pages");
+    p.n_free = int32_of(free_pages, "free_pages"); p.total_new = integer(a[6]);
     p.seq_lens = ints(a[0], "seq_lens", {B}); p.new_lens = ints(a[1], "new_lens", {B}); p.free_pages = ints(a[2], "free_pages", {free_pages});
     p.block_table = (int32_t*)table.data_ptr();
     p.lens_out = ints(a[7], "lens", {B}); p.cu_new = ints(a[8], "cu_new", {B + 1}); p.slot = ints(a[9], "slot", {p.total_new}); p.taken = ints(a[10], "taken", {2});
@@ -394,8 +401,8 @@ PyObject* attn_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
     p.slot = (const int32_t*)given(a[14], at::kInt, "slot", {B, W, ND});
     p.out = given(a[15], at::kBFloat16, "out", {B, W, Hq, d});
     p.lse_out = (float*)given(a[16], at::kFloat, "lse_out", {B, W, Hq});
-    p.B = (int32_t)B; p.W = (int32_t)W; p.Hq = (int32_t)Hq; p.Hkv = (int32_t)Hkv; p.d = (int32_t)d; p.ND = (int32_t)ND; p.u = (int32_t)integer(a[7]);
-    p.page_size = (int32_t)page; p.max_pages = (int32_t)table.size(1); p.n_pages = (int32_t)pages; p.prefix_L = (int32_t)prefix_L; p.max_L = (int32_t)max_L;
+    p.B = (int32_t)B; p.W = (int32_t)W; p.Hq = (int32_t)Hq; p.Hkv = (int32_t)Hkv; p.d = (int32_t)d; p.ND = (int32_t)ND; p.u = int32_of(integer(a[7]), "u");
+    p.page_size = (int32_t)page; p.max_pages = int32_of(table.size(1), "block_table"); p.n_pages = (int32_t)pages; p.prefix_L = (int32_t)prefix_L; p.max_L = (int32_t)max_L;
     p.kv_type = fp8 ? GR_KV_FP8 : GR_KV_BF16;
     p.sm_scale = (float)real(a[8]); p.k_scale = (float)real(a[12]); p.v_scale = (float)real(a[13]);
     p.q = q.data_ptr();
@@ -444,8 +451,8 @@ PyObject* adjust(PyObject*, PyObject* const* a, Py_ssize_t n) {
     p.allowed = (const uint32_t*)given(a[10], at::kInt, "allowed", {masks, (V + 31) / 32});
     p.allowed_row = (const int32_t*)given(a[11], at::kInt, "allowed_row", {B, W});
     p.out = (float*)given(a[12], at::kFloat, "out", {B, W, V});
-    p.B = (int32_t)B; p.W = (int32_t)W; p.V = (int32_t)V; p.depth = (int32_t)depth; p.step = (int32_t)integer(a[1]);
-    p.n_history = (int32_t)rows; p.n_allowed = (int32_t)masks;
+    p.B = (int32_t)B; p.W = (int32_t)W; p.V = (int32_t)V; p.depth = (int32_t)depth; p.step = int32_of(integer(a[1]), "step");
+    p.n_history = int32_of(rows, "history"); p.n_allowed = int32_of(masks, "allowed");
     void* stream = on.stream(a[13]);
     return status_of([&] { return p_adjust(&p, stream); });
   });

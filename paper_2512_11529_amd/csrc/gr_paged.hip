@@ -456,9 +456,10 @@ size_t paged_workspace(const gr_attn_paged_params* p, const PagedPlan& plan) {
   return gr_align256(rows * p->d * 4) + gr_align256(rows * 8);
 }
 
+constexpr int64_t kMaxKeys = (int64_t)1 << 30;               // request_of_rank looks no further (a table may name the same page again and again)
 bool shapes_ok(const gr_attn_paged_params* p) {
   return p->B > 0 && p->W > 0 && p->Hq > 0 && p->Hkv > 0 && p->d > 0 && p->Hq % p->Hkv == 0 && p->page_size > 0 && p->prefix_L >= 0 && p->max_L >= 0 &&
-         (int64_t)p->prefix_L + p->max_L < ((int64_t)1 << 31) - 1024;
+         (int64_t)p->prefix_L + p->max_L < kMaxKeys;
 }
 
 template <auto KERNEL, class... Args>
@@ -478,7 +479,7 @@ extern "C" size_t gr_beam_attn_paged_workspace_bytes(const gr_attn_paged_params*
 extern "C" gr_status gr_beam_attn_paged(const gr_attn_paged_params* p, void* workspace, size_t workspace_bytes, void* stream_) {
   const hipStream_t stream = (hipStream_t)stream_;
   if (!p || p->prefix_L < 0 || p->max_L < 0) return GR_ERR_INVALID_ARG;
-  if ((int64_t)p->prefix_L + p->max_L >= ((int64_t)1 << 31) - 1024) return GR_ERR_UNSUPPORTED;
+  if ((int64_t)p->prefix_L + p->max_L >= kMaxKeys) return GR_ERR_UNSUPPORTED;
   if (!shapes_ok(p)) return GR_ERR_INVALID_ARG;
   if (p->ND < 0 || p->u < 0 || p->u > p->ND || p->max_pages < 0 || p->n_pages < 0) return GR_ERR_INVALID_ARG;
   if (p->kv_type != GR_KV_BF16 && p->kv_type != GR_KV_FP8) return GR_ERR_INVALID_ARG;

@@ -180,7 +180,7 @@ def test_serving(W, Hq, Hkv, d, fp8):
                 fin = np.isfinite(y) & live[b][:, None]
                 # five roundings of half a step, of values that are no larger than 64 between them
                 assert np.abs(logits[b].cpu().numpy()).max() < 16
-                assert np.abs(z.astype(np.float64)[fin] - y[fin]).max(initial=0) <= 5 * 2.0 ** -24 * 64
+                assert np.abs(z[fin].astype(np.float64) - y[fin]).max(initial=0) <= 5 * 2.0 ** -24 * 64
                 assert np.array_equal(inplace[b].cpu().numpy()[live[b]], z[live[b]])
             want = oracle.beam_select(catalogue, inplace.cpu().numpy(), st["scores"].cpu().numpy(), st["prefix"].cpu().numpy(), step)
             assert_select_equal({k: x.cpu().numpy() for k, x in nxt.items()}, want, f"step {step}")

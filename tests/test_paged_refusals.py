@@ -67,7 +67,7 @@ def test_write(gr, change, status):
     (dict(prefix_pages=None), -1), (dict(block_table=None), -1), (dict(seq_lens=None), -1), (dict(k_unshared=None), -1), (dict(max_L=129), -1), (dict(q=A + 8), -1), (dict(v_pages=A + 2), -1),
     (dict(block_table=A + 2), -1), (dict(lse_out=A + 1), -1), (dict(slot=A + 3), -1),
     (dict(d=96), -2), (dict(page_size=8, max_pages=16), -2), (dict(page_size=48), -2), (dict(prefix_L=24), -2), (dict(n_pages=2 ** 27), -2), (dict(Hkv=2048, Hq=2048), -2), (dict(W=2 ** 21), -2),
-    (dict(page_size=1024, max_pages=2 ** 21, max_L=2 ** 31 - 1024, prefix_L=1024), -2)])
+    (dict(page_size=1024, max_pages=2 ** 21, max_L=2 ** 31 - 1024, prefix_L=1024), -2), (dict(page_size=1024, max_pages=2 ** 20, max_L=2 ** 30 - 1024, prefix_L=1024), -2)])
 def test_attn(gr, change, status):
     lib, p = gr.load_library(), ATTN(**{**GOOD_ATTN, **change})
     assert lib.gr_beam_attn_paged(ctypes.byref(p), A, 1 << 40, None) == status
@@ -88,7 +88,7 @@ def test_attn_workspace(gr):
 @pytest.mark.parametrize("change,status", [
     (dict(B=0), -1), (dict(W=0), -1), (dict(V=0), -1), (dict(depth=0), -1), (dict(step=3), -1), (dict(step=-1), -1), (dict(n_history=-1), -1), (dict(n_allowed=-1), -1), (dict(logits=None), -1),
     (dict(out=None), -1), (dict(cu_history=None), -1), (dict(history=None), -1), (dict(prefix=None), -1), (dict(bias_rows=3), -1), (dict(allowed=None), -1), (dict(n_allowed=0), -1),
-    (dict(out=A + 4), -1), (dict(out=A - 4), -1), (dict(logits=A + 1), -1), (dict(allowed=A + 2), -1), (dict(V=32769), -2), (dict(depth=9), -2), (dict(B=1 << 20, W=1 << 12, out=1 << 60), -2),
+    (dict(out=A + 4), -1), (dict(out=A - 4), -1), (dict(logits=A + 1), -1), (dict(allowed=A + 2), -1), (dict(V=32769), -2), (dict(depth=9), -2), (dict(n_history=2 ** 28), -2), (dict(B=1 << 20, W=1 << 12, out=1 << 60), -2),
     (dict(out=A, repetition=None, bias=None, allowed=None, allowed_row=None), 0)])
 def test_adjust(gr, change, status):
     assert gr.load_library().gr_logits_adjust(ctypes.byref(ADJUST(**{**GOOD_ADJUST, **change})), None) == status
@@ -147,6 +147,10 @@ def test_types_shapes_and_strides(gr):
         with pytest.raises(gr.GrError) as e:
             call(**bad)
         assert e.value.status == status, bad
+    with pytest.raises(ValueError, match="page_size: 4294967312 does not fit"):
+        gr.gr_page_map(i(2), i(2), i(5), i(2, 4), 2 ** 32 + 16, 8, 4)
+    with pytest.raises(ValueError, match="step: 4294967296 does not fit"):
+        gr.gr_logits_adjust(f(1, 2, 40), 2 ** 32, bias=f(40), prefix=i(1, 2, 3))
     with pytest.raises(ValueError, match="prefix: expected shape"):
         gr.gr_logits_adjust(f(1, 2, 40), 1, prefix=i(1, 2, 2), history=i(5, 3), cu_history=i(2), repetition=f(1))
     with pytest.raises(ValueError, match="allowed: expected shape"):
