@@ -17,7 +17,7 @@ namespace {
 template <int D, int NCB, int NWAVES, bool CAUSAL, bool KV8, int KS, bool FIND>
 __global__ void __launch_bounds__(NWAVES * 64 * KS) __attribute__((amdgpu_waves_per_eu(NCB == 1 ? 2 : 1, NCB == 1 ? 2 : 1)))
 k_beam_attn(AttnCtx c) {
-  constexpr bool PAGED = false;
+  constexpr bool PAGED = false, WHOLE = false;
 #include "gr_attn_rows.inc"
 }
 

@@ -287,8 +287,8 @@ __device__ __forceinline__ void few_rows(const AttnCtx& c, const unsigned id) {
 constexpr int paged_mix_lds_bytes(int d) { return attn_lds_bytes(d, 128, 1) > paged_few_lds_bytes(d) ? attn_lds_bytes(d, 128, 1) : paged_few_lds_bytes(d); }
 
 // All rows by blocks of 128 or 256; all by blocks of 32; the prefix by blocks of 128 of all requests' rows, which are dealt first (arguments c), and each request's
-// list by blocks of 32 (arguments few).
-template <int D, int NWAVES, bool KV8, int KS, bool FIND>
+// list by blocks of 32 (arguments few).  WHOLE: pages of 64 tokens and more.
+template <int D, int NWAVES, bool KV8, int KS, bool FIND, bool WHOLE>
 __global__ void __launch_bounds__(NWAVES * 64 * KS) __attribute__((amdgpu_waves_per_eu(2, 2))) k_paged_attn(AttnCtx c) {
   constexpr int NCB = 1;
   constexpr bool CAUSAL = false, PAGED = true;
@@ -298,7 +298,7 @@ template <int D, bool KV8>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, D == 64 ? 4 : 2))) k_paged_few(AttnCtx c) {
   few_rows<D, KV8, 0>(c, blockIdx.x);
 }
-template <int D, bool KV8>
+template <int D, bool KV8, bool WHOLE>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) k_paged_mix(AttnCtx c, AttnCtx few, unsigned blocks0) {
   if (blockIdx.x >= blocks0) {
     few_rows<D, KV8, 1>(few, blockIdx.x - blocks0);
@@ -540,20 +540,21 @@ extern "C" gr_status gr_beam_attn_paged(const gr_attn_paged_params* p, void* wor
     c.part_ml = c0.part_ml + first * 2;
     j.part_o = c0.part_o; j.part_ml = c0.part_ml;
   }
-  auto rows = [&](auto dim, auto fp8) -> gr_status {
+  auto rows = [&](auto dim, auto fp8, auto whole) -> gr_status {
     constexpr int D = decltype(dim)::value;
-    constexpr bool K8 = decltype(fp8)::value;
-    if (pack) return launch<k_paged_mix<D, K8>>(paged_mix_lds_bytes(D), 256, grid, stream, c0, c, blocks0);
+    constexpr bool K8 = decltype(fp8)::value, WH = decltype(whole)::value;
+    if (pack) return launch<k_paged_mix<D, K8, WH>>(paged_mix_lds_bytes(D), 256, grid, stream, c0, c, blocks0);
     if (plan.rows == 32) return launch<k_paged_few<D, K8>>(paged_few_lds_bytes(D), 256, grid, stream, c);
-    if (plan.ks == 2) return launch<k_paged_attn<D, 4, K8, 2, false>>(attn_lds_bytes(D, 128, 2), 512, grid, stream, c);
+    if (plan.ks == 2) return launch<k_paged_attn<D, 4, K8, 2, false, WH>>(attn_lds_bytes(D, 128, 2), 512, grid, stream, c);
     if (plan.rows == 128) {
-      if (plan.find) return launch<k_paged_attn<D, 4, K8, 1, true>>(attn_lds_bytes(D, 128, 1), 256, grid, stream, c);
-      return launch<k_paged_attn<D, 4, K8, 1, false>>(attn_lds_bytes(D, 128, 1), 256, grid, stream, c);
+      if (plan.find) return launch<k_paged_attn<D, 4, K8, 1, true, WH>>(attn_lds_bytes(D, 128, 1), 256, grid, stream, c);
+      return launch<k_paged_attn<D, 4, K8, 1, false, WH>>(attn_lds_bytes(D, 128, 1), 256, grid, stream, c);
     }
-    if (plan.find) return launch<k_paged_attn<D, 8, K8, 1, true>>(attn_lds_bytes(D, 256, 1), 512, grid, stream, c);
-    return launch<k_paged_attn<D, 8, K8, 1, false>>(attn_lds_bytes(D, 256, 1), 512, grid, stream, c);
+    if (plan.find) return launch<k_paged_attn<D, 8, K8, 1, true, WH>>(attn_lds_bytes(D, 256, 1), 512, grid, stream, c);
+    return launch<k_paged_attn<D, 8, K8, 1, false, WH>>(attn_lds_bytes(D, 256, 1), 512, grid, stream, c);
   };
-  auto of_type = [&](auto dim) { return kv8 ? rows(dim, std::true_type()) : rows(dim, std::false_type()); };
+  auto of_page = [&](auto dim, auto fp8) { return p->page_size >= KT ? rows(dim, fp8, std::true_type()) : rows(dim, fp8, std::false_type()); };
+  auto of_type = [&](auto dim) { return kv8 ? of_page(dim, std::true_type()) : of_page(dim, std::false_type()); };
   if (const gr_status st = p->d == 128 ? of_type(std::integral_constant<int, 128>()) : of_type(std::integral_constant<int, 64>())) return st;
   if (j.part_o) {
     if (p->d == 128) hipLaunchKernelGGL((k_paged_join<128>), dim3((unsigned)join), dim3(256), 0, stream, j);

@@ -21,11 +21,11 @@ def paged(code_objects):  # noqa: F811
 def test_kernels_over_bf16_pages_keep_their_vectors_in_registers(paged):
     seen = 0
     for name, notes in paged[1].items():
-        # k_paged_attn<D, NWAVES, KV8, ..>, k_paged_few<D, KV8>, k_paged_mix<D, KV8>, k_paged_join<D>
+        # k_paged_attn<D, NWAVES, KV8, KS, FIND, WHOLE>, k_paged_few<D, KV8>, k_paged_mix<D, KV8, WHOLE>, k_paged_join<D>
         if re.search(r"k_paged_attnILi\d+ELi\d+ELb0|k_paged_(few|mix)ILi\d+ELb0|k_paged_join", name):
             seen += 1
             assert re.search(r"\.vgpr_spill_count:\s+0\b", notes) and re.search(r"\.private_segment_fixed_size:\s+0\b", notes), name
-    assert seen == 16           # five, few and mix for both sizes of a head, and two of the join
+    assert seen == 28           # ten, few and two of mix for both sizes of a head, and two of the join
 
 
 def test_addresses_in_scalars_are_written_long_before_loads_use_them(paged):
