@@ -350,8 +350,8 @@ gr_status gr_page_write(const gr_page_write_params* p, void* stream);
  * What a table holds beyond a request's pages is not read; a page number outside [0, n_pages) is read as page 0, and a length outside [0, max_L] as the
  * nearer end.  Slots of a page behind a request's last token may hold anything.
  * GR_KV_FP8: pools of E4M3 codes, scales applied as in gr_beam_attn_fp8kv.
- * Supported: d in {64, 128}; Hq % Hkv == 0; 0 <= u <= ND; prefix_L a multiple of page_size; n_pages * page_size below 2^31; prefix_L + max_L below 2^30;
- * Hkv * d <= 65536; W * Hq/Hkv < 2^22.  bf16 tensors and pools 16-byte aligned; finite values in the slots that are read; |v| * 2^8 * (number of keys) below 2^128.
+ * Supported: d in {64, 128}; Hq % Hkv == 0; 0 <= u <= ND; prefix_L a multiple of page_size; n_pages * page_size below 2^31, and that times
+ * Hkv * d below 2^41; prefix_L + max_L below 2^30; Hkv * d <= 65536; W * Hq/Hkv < 2^22.  bf16 tensors and pools 16-byte aligned; finite values in the slots that are read; |v| * 2^8 * (number of keys) below 2^128.
  * Workspace (device, 256-byte aligned, contents unspecified before and after): partial results of segments, where a row's keys are split.
  * Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE_TOO_SMALL, HIP. */
 typedef struct {

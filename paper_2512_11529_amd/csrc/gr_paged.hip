@@ -498,6 +498,7 @@ extern "C" gr_status gr_beam_attn_paged(const gr_attn_paged_params* p, void* wor
   if (p->page_size < 16 || p->page_size > 1024 || (p->page_size & (p->page_size - 1)) || p->prefix_L % p->page_size) return GR_ERR_UNSUPPORTED;
   const int64_t g = p->Hq / p->Hkv;
   if ((int64_t)p->n_pages * p->page_size >= ((int64_t)1 << 31)) return GR_ERR_UNSUPPORTED;
+  if ((int64_t)p->n_pages * p->page_size * p->Hkv * p->d >= ((int64_t)1 << 41)) return GR_ERR_UNSUPPORTED;      // (a page's address in 32 bits of 1 KiB)
   if ((int64_t)p->Hkv * p->d > 65536 || p->W * g >= ((int64_t)1 << 22)) return GR_ERR_UNSUPPORTED;          // row numbers go through small_div, whose bound is 2^22
   if ((int64_t)p->W * p->Hq * p->d >= ((int64_t)1 << 31) || (int64_t)p->W * p->ND * p->Hkv * p->d >= ((int64_t)1 << 31)) return GR_ERR_UNSUPPORTED;
 

@@ -66,7 +66,7 @@ def test_write(gr, change, status):
     (dict(n_pages=0), -1), (dict(kv_type=7), -1), (dict(sm_scale=0.0), -1), (dict(sm_scale=NAN), -1), (dict(kv_type=1, k_scale=INF), -1), (dict(q=None), -1), (dict(out=None), -1), (dict(k_pages=None), -1),
     (dict(prefix_pages=None), -1), (dict(block_table=None), -1), (dict(seq_lens=None), -1), (dict(k_unshared=None), -1), (dict(max_L=129), -1), (dict(q=A + 8), -1), (dict(v_pages=A + 2), -1),
     (dict(block_table=A + 2), -1), (dict(lse_out=A + 1), -1), (dict(slot=A + 3), -1),
-    (dict(d=96), -2), (dict(page_size=8, max_pages=16), -2), (dict(page_size=48), -2), (dict(prefix_L=24), -2), (dict(n_pages=2 ** 27), -2), (dict(Hkv=2048, Hq=2048), -2), (dict(W=2 ** 21), -2),
+    (dict(d=96), -2), (dict(page_size=8, max_pages=16), -2), (dict(page_size=48), -2), (dict(prefix_L=24), -2), (dict(n_pages=2 ** 27), -2), (dict(n_pages=2 ** 26, Hkv=64, Hq=64, d=128), -2), (dict(Hkv=2048, Hq=2048), -2), (dict(W=2 ** 21), -2),
     (dict(page_size=1024, max_pages=2 ** 21, max_L=2 ** 31 - 1024, prefix_L=1024), -2), (dict(page_size=1024, max_pages=2 ** 20, max_L=2 ** 30 - 1024, prefix_L=1024), -2)])
 def test_attn(gr, change, status):
     lib, p = gr.load_library(), ATTN(**{**GOOD_ATTN, **change})
