@@ -347,7 +347,7 @@ gr_status gr_page_write(const gr_page_write_params* p, void* stream);
  * the beam's own u tokens, as for gr_beam_attn (with `slot` as for gr_beam_attn_slots, or NULL).  Any part may be empty; a beam
  * without a single key gets out = 0 and lse = -inf.  The prefix is read and multiplied once for the rows of all requests where that is
  * less work than with each request's rows by themselves.
- * What a table holds beyond a request's pages is not read; a page number outside [0, n_pages) is read as page 0, and a length outside [0, max_L] as the
+ * What a table holds beyond a request's pages is of no effect; a page number outside [0, n_pages) is read as page 0, and a length outside [0, max_L] as the
  * nearer end.  Slots of a page behind a request's last token may hold anything.
  * GR_KV_FP8: pools of E4M3 codes, scales applied as in gr_beam_attn_fp8kv.
  * Supported: d in {64, 128}; Hq % Hkv == 0; 0 <= u <= ND; prefix_L a multiple of page_size; n_pages * page_size below 2^31, and that times

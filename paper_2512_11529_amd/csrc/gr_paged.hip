@@ -61,6 +61,11 @@ __device__ __forceinline__ void few_rows(const AttnCtx& c, const unsigned id) {
         (uint32_t)((beam - beam0) * c.Hq + (r - beam * c.g)) * (D * 2) + (uint32_t)(((lane % PPR) ^ T::swz_k(rl)) * 16));
   }
 
+  // ---- page numbers: lane i has that of page window + i of the list.  The first segment's are asked for beside the length, whatever it will be (what a table holds
+  // behind a request's pages is of no use to anybody): the first loads of K wait for one of the two after the other less
+  const int most_pages = (c.front + c.max_L + (1 << c.shift) - 1) >> c.shift;
+  auto numbers_from = [&](int first) { return most_pages > 0 ? page_number(c, bu, first + lane, most_pages - 1) : 0; };
+  int window = 0, numbers = sp == 0 ? numbers_from(0) : 0;
   const int keys = c.front + __builtin_amdgcn_readfirstlane(paged_length(c, (int)bu));
   int chunk = (int)div_by((unsigned)keys + (unsigned)ns - 1u, (unsigned)ns, c.inv_split);
   chunk = (chunk + KT - 1) / KT * KT;
@@ -73,10 +78,8 @@ __device__ __forceinline__ void few_rows(const AttnCtx& c, const unsigned id) {
   const int my_lo = (beam_q - beam0) * c.u;
   const int total = nt + (Ru + FT - 1) / FT;
 
-  // ---- page numbers: lane i has that of page window + i of the list
-  const int mask = (1 << c.shift) - 1, last_tok = seg1 - 1, last_chunk = last_tok & ~(RPC - 1), last_page = last_tok >> c.shift;
-  auto numbers_from = [&](int first) { return nt > 0 ? page_number(c, bu, first + lane, last_page) : 0; };
-  int window = seg0 >> c.shift, numbers = numbers_from(window);
+  const int mask = (1 << c.shift) - 1, last_tok = seg1 - 1, last_chunk = last_tok & ~(RPC - 1);
+  if (sp > 0) { window = seg0 >> c.shift; numbers = numbers_from(window); }
   const uint32_t tok_bytes = (uint32_t)c.Hkv * D * EB, own_bytes = (uint32_t)c.Hkv * D * 2;
   const char* k_base = (const char*)c.ks + (size_t)kvh * D * EB;
   const char* v_base = (const char*)c.vs + (size_t)kvh * D * EB;
