@@ -305,3 +305,12 @@ def test_scores_that_rise_by_more_than_a_float_holds(W, lens, P, d, page, fp8):
         rows = s["k"].view(-1, 2, d)
         rows[at] = (k / s["k_scale"]).clamp(-448, 448).to(torch.float8_e4m3fn).view(torch.uint8) if fp8 else k.bfloat16()
     check(s)
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("Hq,Hkv,d,P", [(8, 2, 128, 0), (4, 1, 64, 0), (8, 2, 64, 128)])
+@pytest.mark.parametrize("lens", [[3000, 1], [0, 0, 5000], [64 * k for k in range(17)], [4000] + [1] * 40, [500 + 13 * b for b in range(64)], [(97 * b) % 900 for b in range(128)],
+                                  [(97 * b) % 900 for b in range(129)], [700] * 100])
+def test_few_rows_of_ragged_lists(lens, Hq, Hkv, d, P, fp8):
+    """Each key is met once, whatever the lengths."""
+    check(make(20 + len(lens), lens, 3, Hq, Hkv, d, 16, P=P, u=2, fp8=fp8))
