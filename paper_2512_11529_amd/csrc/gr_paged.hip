@@ -386,17 +386,18 @@ __global__ void __launch_bounds__(256) k_paged_join(JoinCtx c) {
 struct PagedPlan { int rows, ns[2], ks; bool find; };
 
 // More than 80 rows of a (request, KV head) pair are launched as gr_beam_attn launches them.  For fewer, the cheapest of these is taken, by their estimated time in us: blocks of 32 rows or of 128
-// over the whole list, or the prefix packed, each with 1 to 16 segments.  The estimate of a launch is `start`, and the longer of
+// over the whole list, or the prefix packed, each with 1 to 16 segments.  The estimate of a launch is `start`, and (the fourth root of the sum of the fourth powers: a little more than the longer) of
 //   - what its keys take at `rate`;
 //   - its workgroups' time: `few` + `few_step` for every 128 tokens (blocks of 32), `unit` + `tile1` for every 64 (128; two sets of wavefronts where there is at most one workgroup per CU:
 //     `tile2` for every 128), `shared` + `shared_tile` for every 64 (part 0), times the rounds that an XCD's 32 CUs take them in (`few_per_cu` workgroups to a CU, two of part 0 and 1);
-// and, where there are several segments, `join` and the partials written and read at 3.1 TB/s.  Fitted to 870 random calls of 1 to 128 requests of 10 to 16384 tokens with 1 to 80 rows,
-// 430 of them behind a prefix of 64 to 8192 tokens, each timed in up to 40 ways: the mean call takes 1.04 times the best of them (packed wherever that saves half of the blocks,
-// with segments for about one or two workgroups per CU, 1.07 without a prefix and 1.14 with one), the worst 1.39.
+// and, where there are several segments, `join` and the partials written and read at 2.7 TB/s.  Fitted to 870 random calls of 1 to 128 requests of 10 to 16384 tokens with 1 to 80 rows,
+// 430 of them behind a prefix of 64 to 8192 tokens, each timed in up to 40 ways: the mean call takes 1.03 times the best of them, the worst 1.63, and 120 others 1.047 and 1.35 (packed wherever that saves half of the
+// blocks, with segments for about one or two workgroups per CU, 1.07 without a prefix and 1.14 with one; with the longer of the two times alone 16 requests of 1500-3000 tokens x 8 beams
+// took 49.0 us in one segment each, now 39.7 in two, 64 x 8 of 2 KV heads 46.6, 40.7).
 struct PagedCost { double start, few, few_step, few_per_cu, unit, tile1, tile2, shared, shared_tile, join, rate; };
 constexpr PagedCost kPagedCost[2][2] = {      // [head size 128][FP8]; rate in bytes a us
     {{3.3, 1.5, 1.2, 2.0, 2.0, 1.05, 0.95, 1.5, 0.7, 3.1, 8.0e6}, {3.3, 1.5, 1.4, 2.0, 2.0, 1.05, 0.95, 1.5, 0.8, 3.1, 4.0e6}},
-    {{5.0, 0.5, 2.0, 1e4, 1.7, 1.1, 1.25, 0.5, 0.9, 2.5, 6.9e6}, {5.0, 0.5, 2.2, 1.5, 1.7, 1.4, 1.5, 0.5, 1.0, 2.5, 4.4e6}}};
+    {{0.7, 0.15, 1.9, 1.95, 2.1, 0.9, 1.25, 0.4, 0.9, 1.95, 7.9e6}, {1.5, 2.35, 2.05, 1.6, 4.0, 1.45, 1.35, 1.25, 0.9, 2.2, 5.4e6}}};
 
 PagedPlan plan_paged(const gr_attn_paged_params* p) {
   PagedPlan plan{};
@@ -413,7 +414,7 @@ PagedPlan plan_paged(const gr_attn_paged_params* p) {
     return plan;
   }
   const PagedCost& c = kPagedCost[p->d == 128][kv8];
-  const double partial_us = 2.0 * p->B * p->W * p->Hq * p->d * 4 / 3.1e6, token_bytes = 2.0 * p->Hkv * p->d * (kv8 ? 1 : 2);
+  const double partial_us = 2.0 * p->B * p->W * p->Hq * p->d * 4 / 2.7e6, token_bytes = 2.0 * p->Hkv * p->d * (kv8 ? 1 : 2);
   constexpr int kCounts[] = {1, 2, 3, 4, 6, 8, 12, 16};
   double least = 0;
   auto look_at = [&](int rows, int n0, int n1, int ks, double us) {
@@ -424,17 +425,18 @@ PagedPlan plan_paged(const gr_attn_paged_params* p) {
     plan.rows = rows; plan.ns[0] = n0; plan.ns[1] = n1; plan.ks = ks;
   };
   auto larger = [](double a, double b) { return a > b ? a : b; };
+  auto both = [](double a, double b) { return sqrt(sqrt(a * a * a * a + b * b * b * b)); };
   const int64_t list = (int64_t)p->prefix_L + p->max_L;
   const double list_us = list * p->B * token_bytes / c.rate;
   for (const int n : kCounts) {
     if (n > 1 && n * 96 > list) break;
     const double tiles = (double)parts(parts(list, n), KT);
     const double few = (c.few + c.few_step * tiles / 2) * larger(1.0, parts(pairs * n, 8) * parts(M, 32) / (32 * c.few_per_cu));
-    look_at(32, 0, n, 1, larger(few, list_us));
+    look_at(32, 0, n, 1, both(few, list_us));
     const bool sets = list > KT && pairs * parts(M, 128) * n <= 256;
     const int64_t on_xcd = parts(pairs * n, 8) * parts(M, 128);
     const double unit = sets ? (c.unit + c.tile2 * (double)(((int64_t)tiles + 1) >> 1)) * (double)parts(on_xcd, 32) : (c.unit + c.tile1 * tiles) * larger(1.0, on_xcd / 64.0);
-    look_at(128, 0, n, sets ? 2 : 1, larger(unit, list_us));
+    look_at(128, 0, n, sets ? 2 : 1, both(unit, list_us));
   }
   // packed, as the beams of one request (offsets inside its rows fit 32 bits)
   if (p->prefix_L > 0 && p->B > 1 && all < ((int64_t)1 << 22) && (int64_t)p->B * p->W * p->Hq * p->d < ((int64_t)1 << 31)) {
