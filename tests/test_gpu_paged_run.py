@@ -251,3 +251,60 @@ def test_captured_step_over_growing_prompts():
         at = [a + b for a, b in zip(at, n)]
         assert m["lens"].tolist() == at and m["taken"].tolist()[1] == 0
         pages = pages[m["taken"].tolist()[0]:]
+
+
+def test_two_streams_and_two_graphs_over_one_workspace():
+    """Calls at once on two streams, each with a workspace of its own; then two captured calls that share one, replayed in turn."""
+    B, W, Hq, Hkv, d, P, L = 6, 3, 8, 2, 64, 256, 900
+    g = torch.Generator().manual_seed(9)
+    bf = lambda *n: torch.randn(n, generator=g).bfloat16().to(DEV)
+    n_pages, max_pages = 400, 64
+    pools = bf(n_pages, PAGE, Hkv, d), bf(n_pages, PAGE, Hkv, d)
+    prefix = torch.arange(P // PAGE, dtype=torch.int32, device=DEV)
+    table = torch.randint(0, n_pages, (B, max_pages), generator=g).int().to(DEV)
+    states = []
+    for lens in ([L, 0, 17, 300, 64, 899], [5, 700, 1, 128, 900, 33]):
+        q = bf(B, W, Hq, d)
+        states.append(dict(q=q, lens=i32(lens), own=(bf(B, W, ND, Hkv, d), bf(B, W, ND, Hkv, d)), out=torch.empty_like(q), x=torch.randn((B, W, 500), generator=g).to(DEV),
+                           y=torch.empty((B, W, 500), device=DEV)))
+    history, cu, rep = dev(np.random.default_rng(2).integers(0, 500, (600, 1)).astype(np.int32)), i32([100 * b for b in range(B + 1)]), torch.full((B,), 1.5, device=DEV)
+
+    def call(s, ws, stream=None):
+        gr.gr_beam_attn_paged(s["q"], *pools, table, s["lens"], *s["own"], 2, 0.125, L, prefix_pages=prefix, prefix_L=P, out=s["out"], workspace=ws, stream=stream)
+        gr.gr_logits_adjust(s["x"], 0, history=history, cu_history=cu, repetition=rep, out=s["y"], stream=stream)
+
+    need = gr.attn_paged_workspace_bytes(B, W, Hq, Hkv, d, L, P)
+    assert need > 0
+    ws = [torch.empty(need, dtype=torch.uint8, device=DEV) for _ in range(2)]
+    want = []
+    for s in states:
+        call(s, ws[0])
+        want.append((s["out"].clone(), s["y"].clone()))
+    torch.cuda.synchronize()
+    same = lambda: all(torch.equal(s["out"], o) and torch.equal(s["y"], y) for s, (o, y) in zip(states, want))
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for rep_ in range(3):
+        for s in states:
+            s["out"].zero_(), s["y"].zero_()
+        torch.cuda.synchronize()
+        for k in range(20):
+            for s, w, stream in zip(states, ws, streams):
+                call(s, w if rep_ else None, stream)
+        torch.cuda.synchronize()
+        assert same()
+    graphs = []
+    for s in states:
+        side = torch.cuda.Stream()
+        with torch.cuda.stream(side):
+            call(s, ws[0])
+        torch.cuda.synchronize()
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            call(s, ws[0])
+    for rep_ in range(3):
+        for s in states:
+            s["out"].zero_(), s["y"].zero_()
+        for graph in graphs[::1 if rep_ % 2 else -1]:
+            graph.replay()
+        torch.cuda.synchronize()
+        assert same()
