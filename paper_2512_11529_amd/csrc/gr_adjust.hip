@@ -4,11 +4,12 @@
 //     y += bias(v);   y = -inf where the beam's mask forbids v
 //
 // c is zero nearly everywhere, so it never meets the stream of logits: the tokens that the history continues a row with go to a list in LDS, equal ones are
-// counted (few against each other, more in bins, 4096 tokens at a time, from the history again where the list is too short for them), and one thread per counted
+// counted (few against each other, more in bins, 4096 at a time, from the history once more where the list is too short for them), and one thread per counted
 // token changes that token alone, before the row is streamed where it is changed in place, behind it where it is copied.  A row that
 // is changed in place without a bias or a mask is not streamed at all, and a workgroup looks through the history for eight such rows at once.
 // Bound: memory, 8 bytes a logit of streamed rows.  8192 rows x 8192 logits copied with a bias and a mask take 103 us (5.2 TB/s); with counters for all
 // tokens in LDS, looked for behind the stream, the history of 200-600 rows cost another 36.
+#include <type_traits>
 #include "gr_internal.hpp"
 
 namespace {
@@ -22,6 +23,8 @@ constexpr int kMaxHistory = 1 << 28;     // (kSparseRows rows that all of them c
 constexpr int kFew = 256;                 // counted against each other
 constexpr int kList = 1024;
 constexpr int kBins = 4096;
+// History rows of a thread on their way at once: 32 x 128 rows of 4096 in place, 0-3000 history rows, 16.5 us with one, 11.3; 35 x 7 of 928 7.3, 5.6.
+constexpr int kAhead = 4;
 
 struct AdjustCtx {
   int W, V, depth, step, words, n_history, n_allowed, tiles, tile;
@@ -63,17 +66,28 @@ struct Counted {
   const size_t row0;
   const int rows, v0, v1;
 
-  // bit r: history row h counts for row0 + r; and its token
-  __device__ __forceinline__ unsigned match(int h, int* token) const {
-    const int32_t* item = c.history + (size_t)(unsigned)h * (unsigned)c.depth;
-    unsigned hit = s.live;
-    for (int t = 0; t < c.step; t++) {
-      const int x = item[t];
+  // History rows h, h + kThreads, ... (U of them, on their way together): bit r: it counts for row0 + r; and the tokens
+  template <int U>
+  __device__ __forceinline__ void match(int h, unsigned (&hit)[U], int (&token)[U]) const {
+    const int32_t* item[U];
 #pragma unroll
-      for (int r = 0; r < R; r++) hit &= x == s.prefix[r][t] ? ~0u : ~(1u << r);
+    for (int u = 0; u < U; u++) {
+      hit[u] = h + u * kThreads < s.h1 ? s.live : 0;
+      item[u] = c.history + (size_t)(unsigned)min(h + u * kThreads, s.h1 - 1) * (unsigned)c.depth;
     }
-    *token = item[c.step];
-    return *token >= v0 && *token < v1 ? hit : 0;
+    for (int t = 0; t < c.step; t++) {
+      int x[U];
+#pragma unroll
+      for (int u = 0; u < U; u++) x[u] = item[u][t];
+#pragma unroll
+      for (int r = 0; r < R; r++)
+#pragma unroll
+        for (int u = 0; u < U; u++) hit[u] &= x[u] == s.prefix[r][t] ? ~0u : ~(1u << r);
+    }
+#pragma unroll
+    for (int u = 0; u < U; u++) token[u] = item[u][c.step];
+#pragma unroll
+    for (int u = 0; u < U; u++) hit[u] = token[u] >= v0 && token[u] < v1 ? hit[u] : 0;
   }
   __device__ __forceinline__ void find() {
     const int tid = (int)threadIdx.x;
@@ -94,21 +108,28 @@ struct Counted {
     __syncthreads();
     const int h1 = s.h1;
     // (wavefront by wavefront: one lane asks for the places of all)
-    for (int h0 = s.h0; h0 < h1; h0 += kThreads) {
-      const int h = h0 + tid;
-      int v = 0;
-      const unsigned hit = h < h1 ? match(h, &v) : 0;
-      if (!__any(hit)) continue;
+    auto look = [&](int h0, auto ahead) {
+      constexpr int U = decltype(ahead)::value;
+      unsigned hit[U];
+      int v[U];
+      match<U>(h0 + tid, hit, v);
 #pragma unroll
-      for (int r = 0; r < R; r++) {
-        const uint64_t all = __ballot((hit >> r) & 1);
-        if (all == 0) continue;
-        int at = 0;
-        if ((tid & 63) == 0) at = atomicAdd(&s.n, __popcll(all));
-        at = __builtin_amdgcn_readfirstlane(at) + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(all >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)all, 0));
-        if (((hit >> r) & 1) && at < kList) s.list[at] = r * kMaxV + v;
+      for (int u = 0; u < U; u++) {
+        if (!__any(hit[u])) continue;
+#pragma unroll
+        for (int r = 0; r < R; r++) {
+          const uint64_t all = __ballot((hit[u] >> r) & 1);
+          if (all == 0) continue;
+          int at = 0;
+          if ((tid & 63) == 0) at = atomicAdd(&s.n, __popcll(all));
+          at = __builtin_amdgcn_readfirstlane(at) + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(all >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)all, 0));
+          if (((hit[u] >> r) & 1) && at < kList) s.list[at] = r * kMaxV + v[u];
+        }
       }
-    }
+    };
+    int h0 = s.h0;
+    for (; h1 - h0 > kThreads; h0 += kThreads * kAhead) look(h0, std::integral_constant<int, kAhead>());
+    if (h0 < h1) look(h0, std::integral_constant<int, 1>());
     __syncthreads();
   }
   template <class F>
@@ -132,27 +153,53 @@ struct Counted {
       }
       return;
     }
-    // only the bins that the history touches are cleared and read
-    for (int r = 0; r < rows; r++) {
-      if (!((s.live >> r) & 1)) continue;
-      for (int base = v0; base < v1; base += kBins) {
-        auto each = [&](auto&& g) {
-          for (int i = tid; n <= kList && i < n; i += kThreads) {
-            const int v = s.list[i] - r * kMaxV;
-            if (v >= base && v < min(base + kBins, v1)) g(v);
+    if (n <= kList) {                            // only the bins that the list touches are cleared and read
+      for (int r = 0; r < rows; r++) {
+        if (!((s.live >> r) & 1)) continue;
+        for (int base = v0; base < v1; base += kBins) {
+          auto each = [&](auto&& g) {
+            for (int i = tid; i < n; i += kThreads) {
+              const int v = s.list[i] - r * kMaxV;
+              if (v >= base && v < min(base + kBins, v1)) g(v);
+            }
+            __syncthreads();
+          };
+          each([&](int v) { s.bins[v - base] = 0; });
+          each([&](int v) { atomicAdd(&s.bins[v - base], 1u); });
+          each([&](int v) {
+            const uint32_t count = atomicExch(&s.bins[v - base], 0u);
+            if (count) f(r, v, (int)count);
+          });
+        }
+      }
+      return;
+    }
+    // the history once more for as many rows as have room in the bins together, or for each part of one row (4 x 2 rows of 32768, 20000 history rows: 73 us; through it three times for
+    // each part, to clear, count and read only what it touches, 241)
+    const int width = min(v1 - v0, kBins), together = min(kBins / width, R);
+    for (int r0 = 0; r0 < rows; r0 += together) {
+      if (!((s.live >> r0) & ((1u << together) - 1u))) continue;
+      for (int base = v0; base < v1; base += width) {
+        for (int i = tid; i < together * width; i += kThreads) s.bins[i] = 0;
+        __syncthreads();
+        for (int h0 = s.h0; h0 < s.h1; h0 += kThreads * kAhead) {
+          unsigned hit[kAhead];
+          int v[kAhead];
+          match<kAhead>(h0 + tid, hit, v);
+#pragma unroll
+          for (int u = 0; u < kAhead; u++) {
+            if (v[u] < base || v[u] >= base + width) continue;
+            for (int k = 0; k < together; k++)
+              if ((hit[u] >> (r0 + k)) & 1) atomicAdd(&s.bins[k * width + v[u] - base], 1u);
           }
-          for (int h = s.h0 + tid; n > kList && h < s.h1; h += kThreads) {
-            int v;
-            if (((match(h, &v) >> r) & 1) && v >= base && v < base + kBins) g(v);
+        }
+        __syncthreads();
+        for (int k = 0; k < together; k++)
+          for (int i = (s.live >> (r0 + k)) & 1 ? tid : width; i < width; i += kThreads) {
+            const uint32_t count = s.bins[k * width + i];
+            if (count) f(r0 + k, base + i, (int)count);
           }
-          __syncthreads();
-        };
-        each([&](int v) { s.bins[v - base] = 0; });
-        each([&](int v) { atomicAdd(&s.bins[v - base], 1u); });
-        each([&](int v) {
-          const uint32_t count = atomicExch(&s.bins[v - base], 0u);
-          if (count) f(r, v, (int)count);
-        });
+        __syncthreads();
       }
     }
   }

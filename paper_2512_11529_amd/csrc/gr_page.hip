@@ -70,7 +70,7 @@ __global__ void __launch_bounds__(kMapThreads) k_page_map(MapCtx c) {
   __syncthreads();
   for (int w = 0; w < wave; w++) { at.x = add_capped(at.x, s_wave[w].x); at.y = add_capped(at.y, s_wave[w].y); }
   const bool writes = blockIdx.x == 0;
-  int refused = 0;
+  int refused = 0, last = 0;
   for (int b = b0; b < b1; b++) {
     uint32_t s, n, need;
     lengths(b, &s, &n, &need);
@@ -86,11 +86,22 @@ __global__ void __launch_bounds__(kMapThreads) k_page_map(MapCtx c) {
       if (b == c.B - 1) c.cu[c.B] = (int)cu1;
     }
     // (pages go out from the first on, and where one request finds too few, so do all behind it that need any: the last one served says how many)
-    if (writes && served && need > 0) atomicMax(&s_last[0], (int)off1);
+    if (served && need > 0) last = (int)off1;
     refused += !served && n > 0;
     at = make_uint2(cu1, off1);
   }
-  if (writes && refused) atomicAdd(&s_last[1], refused);
+  if (writes) {                              // (one lane for all: atomics of 64 lanes are made one after the other; 575 requests of two tokens 10.9 us with them)
+    const uint64_t some = __ballot(last > 0);
+    if (some) last = __builtin_amdgcn_readlane(last, 63 - __clzll((long long)some));
+    if (__any(refused)) {
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) refused += __shfl_xor(refused, d, 64);
+    }
+    if (lane == 0) {
+      if (some) atomicMax(&s_last[0], last);
+      if (refused) atomicAdd(&s_last[1], refused);
+    }
+  }
   __syncthreads();
   if (writes && tid < 2) c.taken[tid] = s_last[tid];
 
