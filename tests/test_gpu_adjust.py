@@ -185,3 +185,11 @@ def test_on_another_stream():
     got = gr.gr_logits_adjust(logits, 0, bias=bias, stream=side)
     torch.cuda.synchronize()
     assert (got == 3.0).all()
+
+
+@pytest.mark.parametrize("inplace", [False, True])
+@pytest.mark.parametrize("B,W,V,hist", [(3, 15, 266, 2500), (1, 9, 64, 5000), (2, 3, 20000, 6000), (1, 8, 2048, 1300), (1, 2, 4097, 4000), (2, 17, 600, 700)])
+def test_more_counted_tokens_than_the_list_holds(B, W, V, hist, inplace):
+    for bias, masks in ((None, 0), (1, 3)):
+        check(make(B * W + V, B, W, V, 2, 0, hist, bias=bias, masks=masks, dead=0.2), inplace)
+    check(make(V, B, W, V, 3, 2, hist, families=2), inplace)

@@ -314,3 +314,11 @@ def test_scores_that_rise_by_more_than_a_float_holds(W, lens, P, d, page, fp8):
 def test_few_rows_of_ragged_lists(lens, Hq, Hkv, d, P, fp8):
     """Each key is met once, whatever the lengths."""
     check(make(20 + len(lens), lens, 3, Hq, Hkv, d, 16, P=P, u=2, fp8=fp8))
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("page", [16, 64])
+@pytest.mark.parametrize("B,W,P,u", [(2, 300, 0, 0), (2, 300, 0, 3), (130, 90, 0, 1), (40, 300, 64, 0), (3, 40, 128, 2)])
+def test_many_rows_without_keys(B, W, P, u, page, fp8):
+    for lens, max_L in (([0] * B, 0), ([0] * B, 200), ([0] * (B - 1) + [5], None)):
+        check(make(B + W, lens, W, 4, 2, 128 if B < 10 else 64, page, P=P, u=u, fp8=fp8, max_L=max_L))
