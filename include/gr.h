@@ -26,6 +26,8 @@
  *     call and synchronises `stream` once to report table errors.
  *   - Return value: GR_OK or a negative gr_status.  Nothing is printed, thrown or aborted.
  *     Host-checkable argument errors are reported before anything is enqueued.
+ *   - The calls around pages and logits (gr_page_*, gr_beam_attn_paged, gr_logits_adjust) report UNSUPPORTED for shapes whose launch would
+ *     have 2^32 threads or more (from 2^24 rows of logits on, or 2^23 blocks of query rows and segments).
  *   - bf16 tensors are raw 16-bit patterns; all tensors are dense, row-major, in the stated shape.
  */
 #ifndef GR_H_

@@ -330,6 +330,7 @@ extern "C" gr_status gr_logits_adjust(const gr_logits_adjust_params* p, void* st
     return GR_ERR_INVALID_ARG;
   if (p->V > kMaxV || p->depth > kMaxDepth || p->n_history >= kMaxHistory) return GR_ERR_UNSUPPORTED;
   const int64_t rows = (int64_t)p->B * p->W;
+  if (rows >= ((int64_t)1 << 31)) return GR_ERR_UNSUPPORTED;
   const uint64_t bytes = (uint64_t)rows * p->V * 4, from = (uint64_t)(uintptr_t)p->logits, to = (uint64_t)(uintptr_t)p->out;
   const bool inplace = from == to;
   if (!inplace && from < to + bytes && to < from + bytes) return GR_ERR_INVALID_ARG;       // out lies across the logits
@@ -347,7 +348,7 @@ extern "C" gr_status gr_logits_adjust(const gr_logits_adjust_params* p, void* st
   c.row_blocks = (unsigned)((p->W + kSparseRows - 1) / kSparseRows);
   const bool sparse = inplace && !p->bias && !p->allowed;
   const int64_t grid = sparse ? (int64_t)p->B * c.row_blocks : rows * c.tiles;
-  if (grid >= ((int64_t)1 << 31)) return GR_ERR_UNSUPPORTED;
+  if (!gr_grid_fits(grid, kThreads)) return GR_ERR_UNSUPPORTED;
   const hipStream_t stream = (hipStream_t)stream_;
 #define GR_LAUNCH(...) hipLaunchKernelGGL((__VA_ARGS__), dim3((unsigned)grid), dim3(kThreads), 0, stream, c)
   if (sparse) GR_LAUNCH(k_logits_penalise);

@@ -25,6 +25,9 @@ static inline gr_status gr_allow_lds(size_t bytes) {
   return GR_OK;
 }
 
+// The size of a launch in threads is a 32-bit number.
+static inline bool gr_grid_fits(int64_t workgroups, int64_t threads) { return workgroups * threads < ((int64_t)1 << 32); }
+
 static inline size_t gr_align256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // ------------------------------------------------------------------ mask blob layout

@@ -270,6 +270,7 @@ extern "C" gr_status gr_page_write(const gr_page_write_params* p, void* stream_)
   const int u = all >= (int64_t)256 * 4 * 512 ? 4 : 1;
   c.rows_wg = (uint32_t)((256 * u + c.pieces - 1) / c.pieces);
   const unsigned grid = (c.T + c.rows_wg - 1) / c.rows_wg;
+  if (!gr_grid_fits(grid, 256)) return GR_ERR_UNSUPPORTED;
 #define GR_LAUNCH(F, U_) hipLaunchKernelGGL((k_page_write<F, U_>), dim3(grid), dim3(256), 0, stream, c)
   auto ordinary = [](float s) { return s >= 0x1p-60f && s <= 0x1p60f; };
   const int type = !fp8 ? 0 : ordinary(p->k_scale) && ordinary(p->v_scale) ? 1 : 2;

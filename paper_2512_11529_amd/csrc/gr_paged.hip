@@ -529,7 +529,7 @@ extern "C" gr_status gr_beam_attn_paged(const gr_attn_paged_params* p, void* wor
     AttnCtx& x = k == 0 ? c0 : c;
     const int64_t groups = (int64_t)x.B * x.Hkv * x.nsplit;
     blocks[k] = (groups + 7) / 8 * 8 * x.MB;
-    if (groups >= ((int64_t)1 << 31) || blocks[0] + blocks[1] >= ((int64_t)1 << 31)) return GR_ERR_UNSUPPORTED;
+    if (groups >= ((int64_t)1 << 31) || !gr_grid_fits(blocks[0] + blocks[1], plan.rows == 256 || plan.ks == 2 ? 512 : 256)) return GR_ERR_UNSUPPORTED;
     x.n_groups = (int)groups; x.inv_mb = div_inv((uint32_t)x.MB); x.inv_split = div_inv((uint32_t)x.nsplit);
   }
   const unsigned grid = (unsigned)(blocks[0] + blocks[1]), blocks0 = (unsigned)blocks[0];
@@ -538,7 +538,7 @@ extern "C" gr_status gr_beam_attn_paged(const gr_attn_paged_params* p, void* wor
   if (const size_t need = paged_workspace(p, plan)) {
     if (!workspace || ((uintptr_t)workspace & 255)) return GR_ERR_INVALID_ARG;
     if (workspace_bytes < need) return GR_ERR_WORKSPACE_TOO_SMALL;
-    if (join >= ((int64_t)1 << 31)) return GR_ERR_UNSUPPORTED;
+    if (!gr_grid_fits(join, 256)) return GR_ERR_UNSUPPORTED;
     const size_t rows = (size_t)p->B * p->W * p->Hq, first = rows * plan.ns[0];          // part 1's partials lie behind part 0's
     c0.part_o = (float*)workspace;
     c0.part_ml = (float*)((char*)workspace + gr_align256(rows * (plan.ns[0] + plan.ns[1]) * p->d * 4));

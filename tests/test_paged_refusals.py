@@ -159,3 +159,15 @@ def test_types_shapes_and_strides(gr):
         gr.gr_logits_adjust(f(2, 2, 40), 0, bias=f(3, 40))
     with pytest.raises(gr.GrError):
         gr.gr_logits_adjust(f(1, 2, 40), 0, repetition=f(1))       # a penalty without a history
+
+
+def test_launches_of_too_many_threads(gr):
+    """2^32 threads and more are refused before anything is enqueued."""
+    lib = gr.load_library()
+    far = 1 << 60
+    for change in (dict(B=8192, W=2048, V=32, out=far), dict(B=8192, W=2048, V=1, out=A), dict(B=1 << 24, W=8, V=1, out=A, bias=None, allowed=None, allowed_row=None),
+                   dict(B=2 ** 31 - 1, W=2 ** 31 - 1, V=32768, out=far), dict(B=1 << 30, W=1 << 30, V=32768, out=A)):
+        assert lib.gr_logits_adjust(ctypes.byref(ADJUST(**{**GOOD_ADJUST, **change})), None) == -2, change
+    for change in (dict(B=1 << 21, W=1, Hq=8, Hkv=8), dict(B=1 << 21, W=1, Hq=8, Hkv=8, prefix_L=0), dict(B=1 << 14, W=1 << 14, Hq=8, Hkv=8)):
+        assert lib.gr_beam_attn_paged(ctypes.byref(ATTN(**{**GOOD_ATTN, **change})), A, 1 << 40, None) == -2, change
+    assert lib.gr_page_write(ctypes.byref(WRITE(**{**GOOD_WRITE, "T": 2 ** 31 - 1, "Hkv": 64, "d": 128, "k_stride": 8192, "v_stride": 8192})), None) == -2
