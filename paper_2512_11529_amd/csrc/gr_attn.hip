@@ -105,6 +105,18 @@ bool attn_wants_order(const gr_attn_params* p, const AttnPlan& plan) {
   return p->B >= 2 && p->B <= kMaxOrderB && p->total_L != (int64_t)p->B * p->max_L && plan.many;
 }
 
+int g_plan_rows = 0, g_plan_segments = 0;                  // gr_diag_attn_plan: 0 = use the rule
+AttnPlan plan_of(const gr_attn_params* p, bool kv8) {
+  if (!g_plan_rows) return plan_attn(p, kv8);
+  const int64_t cap = p->max_L / KT, M = (int64_t)p->W * (p->Hq / p->Hkv);       // a sweep asked for this tiling; keep at least one tile per segment
+  AttnPlan plan;
+  plan.mwg = g_plan_rows;
+  plan.nsplit = (int)(g_plan_segments < cap ? g_plan_segments : (cap < 1 ? 1 : cap));
+  plan.ks = sets_of(p, plan);
+  plan.many = (int64_t)p->B * p->Hkv * ((M + plan.mwg - 1) / plan.mwg) * plan.nsplit > 256;
+  return plan;
+}
+
 }  // namespace
 
 extern "C" gr_status gr_diag_attn_plan(int32_t rows_per_workgroup, int32_t l_segments) {
@@ -116,7 +128,7 @@ extern "C" gr_status gr_diag_attn_plan(int32_t rows_per_workgroup, int32_t l_seg
 
 extern "C" size_t gr_beam_attn_workspace_bytes(const gr_attn_params* p) {
   if (!p || p->B <= 0 || p->W <= 0 || p->Hq <= 0 || p->Hkv <= 0 || p->Hq % p->Hkv) return 0;
-  const AttnPlan plan = plan_attn(p, false);               // (what it says about the workspace is the same for FP8 codes)
+  const AttnPlan plan = plan_of(p, false);               // (what it says about the workspace is the same for FP8 codes)
   size_t need = attn_wants_order(p, plan) ? gr_align256((size_t)p->B * 4) : 0;      // (up to kRankB requests: asked for as ever, and not used)
   if (plan.nsplit > 1) {
     const size_t rows = (size_t)p->B * plan.nsplit * p->W * p->Hq;
@@ -153,7 +165,7 @@ gr_status attn_run(const gr_attn_params* p, const int32_t* slot, bool kv8, float
   AttnCtx c;
   c.B = p->B; c.W = p->W; c.Hq = p->Hq; c.Hkv = p->Hkv; c.g = g; c.ND = p->ND; c.u = p->u;
   c.M = p->W * g;
-  const AttnPlan plan = plan_attn(p, kv8);
+  const AttnPlan plan = plan_of(p, kv8);
   c.MB = (c.M + plan.mwg - 1) / plan.mwg;
   c.nsplit = plan.nsplit;
   c.n_groups = p->B * p->Hkv * c.nsplit;

@@ -148,22 +148,14 @@ __device__ __forceinline__ size_t slot_of(const C& c, unsigned b, int t, int las
 //     16 query and 2 KV heads 93, 103, of 8 and 2 heads of 64 28.3, 32.0.  But 64 x 1500 x 256 425, 421, 32 x 4096 x 256 504, 498, with FP8 codes
 //     128 x 512 x 256 385, 373, and where queries and outputs are twice what the Infinity Cache holds 128 x 128 x 256 of 32 heads 223, 216.
 struct AttnPlan { int mwg, nsplit, ks; bool many; };       // many: more workgroups than CUs before the choice of 128 rows for their own sake
-int g_plan_rows = 0, g_plan_segments = 0;                  // gr_diag_attn_plan: 0 = use the rule below
+int sets_of(const gr_attn_params* p, const AttnPlan& plan) {
+  const int64_t M = (int64_t)p->W * (p->Hq / p->Hkv);
+  return plan.mwg == 128 && p->max_L > KT && (int64_t)p->B * p->Hkv * ((M + 127) / 128) * plan.nsplit <= 256 ? 2 : 1;
+}
 AttnPlan plan_attn(const gr_attn_params* p, bool kv8) {
   const int g = p->Hq / p->Hkv;
   const int64_t M = (int64_t)p->W * g;
   AttnPlan plan;
-  auto wants_sets = [&](const AttnPlan& q) {
-    return q.mwg == 128 && p->max_L > KT && (int64_t)p->B * p->Hkv * ((M + 127) / 128) * q.nsplit <= 256 ? 2 : 1;
-  };
-  if (g_plan_rows) {                                        // a sweep asked for this tiling; keep at least one tile per segment
-    const int64_t cap = p->max_L / KT;
-    plan.mwg = g_plan_rows;
-    plan.nsplit = (int)(g_plan_segments < cap ? g_plan_segments : (cap < 1 ? 1 : cap));
-    plan.ks = wants_sets(plan);
-    plan.many = (int64_t)p->B * p->Hkv * ((M + plan.mwg - 1) / plan.mwg) * plan.nsplit > 256;
-    return plan;
-  }
   const int64_t units256 = (int64_t)p->B * p->Hkv * ((M + 255) / 256);
   plan.mwg = (M <= 128 || units256 < 256) ? 128 : 256;     // 256-row workgroups only when they fill the chip by themselves
   const int64_t units = (int64_t)p->B * p->Hkv * ((M + plan.mwg - 1) / plan.mwg);
@@ -188,7 +180,7 @@ AttnPlan plan_attn(const gr_attn_params* p, bool kv8) {
     const bool short_prompts = !kv8 && p->total_L <= (int64_t)p->B * 1024 && units256 > 256 && (int64_t)p->B * p->W * p->Hq * p->d * 4 <= ((int64_t)400 << 20);
     if (fewer_rows || short_prompts) plan.mwg = 128;
   }
-  plan.ks = wants_sets(plan);
+  plan.ks = sets_of(p, plan);
   return plan;
 }
 

@@ -171,3 +171,16 @@ def test_launches_of_too_many_threads(gr):
     for change in (dict(B=1 << 21, W=1, Hq=8, Hkv=8), dict(B=1 << 21, W=1, Hq=8, Hkv=8, prefix_L=0), dict(B=1 << 14, W=1 << 14, Hq=8, Hkv=8)):
         assert lib.gr_beam_attn_paged(ctypes.byref(ATTN(**{**GOOD_ATTN, **change})), A, 1 << 40, None) == -2, change
     assert lib.gr_page_write(ctypes.byref(WRITE(**{**GOOD_WRITE, "T": 2 ** 31 - 1, "Hkv": 64, "d": 128, "k_stride": 8192, "v_stride": 8192})), None) == -2
+
+
+def test_a_forced_plan_is_of_the_packed_cache_alone(gr):
+    lib = gr.load_library()
+    shape = dict(B=3, W=100, Hq=8, Hkv=2, d=64, max_L=5000)
+    free = gr.attn_paged_workspace_bytes(**shape), gr.attn_workspace_bytes(**shape)
+    assert lib.gr_diag_attn_plan(256, 2) == 0
+    try:
+        forced = gr.attn_paged_workspace_bytes(**shape), gr.attn_workspace_bytes(**shape)
+    finally:
+        assert lib.gr_diag_attn_plan(0, 0) == 0
+    assert forced[0] == free[0] > 0 and forced[1] != free[1]
+    assert (gr.attn_paged_workspace_bytes(**shape), gr.attn_workspace_bytes(**shape)) == free
