@@ -430,6 +430,10 @@ gr_status gr_logits_adjust(const gr_logits_adjust_params* p, void* stream);
  *   workgroups of `rows_per_workgroup` (128 or 256) query rows and `l_segments` (1..16, lowered to the number of
  *   K/V tiles in the longest prompt) prompt segments instead of the built-in launch rule; (0, 0) restores the rule.
  *   For sweeps that refit the rule; not thread-safe against concurrent gr_beam_attn calls.
+ * gr_diag_attn_paged_plan: host only.  How gr_beam_attn_paged launches a call of these shapes (of what gr_beam_attn_paged_workspace_bytes looks at), as five
+ *   numbers in host memory: query rows of a workgroup that meets requests' own lists (32, 128 or 256), segments of the prefix where the rows of all requests
+ *   meet it together (0: every row walks its whole list), segments of a list, sets of wavefronts of a workgroup (1 or 2), and 1 where workgroups look for
+ *   the longest request first.  For tests that have to reach every kernel.
  * gr_diag_issue_loop: the issue test behind the attention kernel's roofline discussion.  `workgroups` x 8 wavefronts
  *   (256 workgroups = two wavefronts per SIMD, 512 = four) each run `iters` x 4 slots of { one bf16 32x32x16 MFMA if
  *   `with_mfma`, `n_fma` independent fp32 FMAs, `n_exp` v_exp_f32 }.  Built combinations (n_fma, n_exp): (0,0) (2,0)
@@ -446,6 +450,7 @@ gr_status gr_diag_issue_loop(const void* operands, int32_t workgroups, int32_t i
 gr_status gr_diag_issue_loop_lds(const void* operands, int32_t workgroups, int32_t rounds, int32_t n_fma, int32_t n_exp,
                                  int32_t lds_every, void* sink, void* stream);
 gr_status gr_diag_attn_plan(int32_t rows_per_workgroup, int32_t l_segments);
+gr_status gr_diag_attn_paged_plan(const gr_attn_paged_params* p, int32_t* plan);
 gr_status gr_diag_stream_read(const void* src, size_t bytes, void* sink, void* stream);
 gr_status gr_diag_mfma_loop(const void* operands, int32_t workgroups, int32_t iters, void* sink, void* stream);
 double    gr_diag_mfma_flops(int32_t workgroups, int32_t iters);

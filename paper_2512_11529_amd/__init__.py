@@ -25,7 +25,7 @@ from . import build as _build
 __all__ = ["load_library", "gr_beam_attn", "gr_beam_attn_fp8kv", "gr_prefill_attn", "gr_item_mask_build", "gr_beam_select", "gr_beam_select_noalloc", "gr_beam_reorder",
            "gr_status_string",
            "attn_workspace_bytes", "select_workspace_bytes", "GrError", "GR_SELECT_FORCE_DENSE", "LIB_PATH",
-           "gr_diag_stream_read", "gr_diag_mfma_loop", "gr_diag_attn_plan", "gr_diag_issue_loop", "gr_diag_issue_loop_lds", "gr_beam_attn_slots", "gr_beam_slot_update",
+           "gr_diag_stream_read", "gr_diag_mfma_loop", "gr_diag_attn_plan", "gr_diag_attn_paged_plan", "gr_diag_issue_loop", "gr_diag_issue_loop_lds", "gr_beam_attn_slots", "gr_beam_slot_update",
            "gr_page_map", "gr_page_write", "gr_beam_attn_paged", "attn_paged_workspace_bytes", "gr_logits_adjust"]
 
 LIB_PATH = _build.LIB_PATH
@@ -135,6 +135,8 @@ def load_library(path: str = None):
     lib.gr_beam_attn_paged.argtypes = [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]
     lib.gr_beam_attn_paged_workspace_bytes.restype = ctypes.c_size_t
     lib.gr_beam_attn_paged_workspace_bytes.argtypes = [ctypes.c_void_p]
+    lib.gr_diag_attn_paged_plan.restype = ctypes.c_int32
+    lib.gr_diag_attn_paged_plan.argtypes = [ctypes.c_void_p, ctypes.c_void_p]
     _lib, _native = lib, None            # (the marshalling module binds to this library at its next call)
     return lib
 
@@ -386,9 +388,14 @@ def gr_page_write(k, v, slot, k_pages, v_pages, k_scale=1.0, v_scale=1.0, stream
 
 def attn_paged_workspace_bytes(B, W, Hq, Hkv, d, max_L, prefix_L=0, fp8=False, page_size=16) -> int:
     """Workspace bytes of gr_beam_attn_paged (the same for pages of any size)."""
+    p = _paged_shapes(B, W, Hq, Hkv, d, max_L, prefix_L, fp8, page_size)
+    return int(load_library().gr_beam_attn_paged_workspace_bytes(ctypes.byref(p)))
+
+
+def _paged_shapes(B, W, Hq, Hkv, d, max_L, prefix_L, fp8, page_size):
     p = _AttnPagedParams()
     p.B, p.W, p.Hq, p.Hkv, p.d, p.max_L, p.prefix_L, p.kv_type, p.page_size = B, W, Hq, Hkv, d, int(max_L), int(prefix_L), int(bool(fp8)), int(page_size)
-    return int(load_library().gr_beam_attn_paged_workspace_bytes(ctypes.byref(p)))
+    return p
 
 
 def gr_beam_attn_paged(q, k_pages, v_pages, block_table, seq_lens, k_unshared, v_unshared, u, sm_scale, max_L, prefix_pages=None, prefix_L=0, k_scale=1.0,
@@ -430,6 +437,17 @@ def gr_diag_attn_plan(rows_per_workgroup=0, l_segments=0):
     rc = load_library().gr_diag_attn_plan(int(rows_per_workgroup), int(l_segments))
     if rc != 0:
         raise GrError(rc, "gr_diag_attn_plan")
+
+
+def gr_diag_attn_paged_plan(B, W, Hq, Hkv, d, max_L, prefix_L=0, fp8=False, page_size=16):
+    """How gr_beam_attn_paged launches such a call: (rows of a workgroup, segments of a prefix met by all requests' rows together or 0, segments of a list, sets of
+    wavefronts, longest request first)."""
+    p = _paged_shapes(B, W, Hq, Hkv, d, max_L, prefix_L, fp8, page_size)
+    plan = (ctypes.c_int32 * 5)()
+    rc = load_library().gr_diag_attn_paged_plan(ctypes.byref(p), plan)
+    if rc != 0:
+        raise GrError(rc, "gr_diag_attn_paged_plan")
+    return tuple(plan[:4]) + (bool(plan[4]),)
 
 
 def gr_diag_issue_loop(operands, workgroups, iters, n_fma, n_exp, with_mfma, sink, stream=None):

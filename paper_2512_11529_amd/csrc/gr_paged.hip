@@ -481,6 +481,13 @@ extern "C" size_t gr_beam_attn_paged_workspace_bytes(const gr_attn_paged_params*
   return paged_workspace(p, plan_paged(p));
 }
 
+extern "C" gr_status gr_diag_attn_paged_plan(const gr_attn_paged_params* p, int32_t* plan) {
+  if (!p || !plan || !shapes_ok(p)) return GR_ERR_INVALID_ARG;
+  const PagedPlan a = plan_paged(p);
+  plan[0] = a.rows; plan[1] = a.ns[0]; plan[2] = a.ns[1]; plan[3] = a.ks; plan[4] = a.find;
+  return GR_OK;
+}
+
 extern "C" gr_status gr_beam_attn_paged(const gr_attn_paged_params* p, void* workspace, size_t workspace_bytes, void* stream_) {
   const hipStream_t stream = (hipStream_t)stream_;
   if (!p || p->prefix_L < 0 || p->max_L < 0) return GR_ERR_INVALID_ARG;
