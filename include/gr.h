@@ -188,8 +188,8 @@ gr_status gr_item_mask_build(const int32_t* items_sorted, int64_t n_items, int32
  *   prefix  int32 [B, W, depth]  tokens chosen so far (entries >= step+1 are -1 on output)
  *   range   int32 [B, W, 2]      table row range [lo, hi) of the prefix
  * Step 0 ignores prefix_in/range_in.  Step 1 reads prefix_in[...,0]; step 2 reads range_in.
- * Behaviour is undefined if logits or scores contain NaN, or if a live beam's prefix/range is not
- * one this mask produced.
+ * Behaviour is undefined if scores or the logits of a live beam contain NaN, or if a live beam's prefix/range is not
+ * one this mask produced.  What the logits of dead beams hold is of no effect.
  *
  * mask == NULL: unconstrained (every token valid); range_out = [0,0), item_index_out = -1.
  * Supported: depth == 3; 1 <= W <= 2048; 1 <= V <= 32768; W*V < 2^31.
@@ -391,7 +391,7 @@ gr_status gr_beam_attn_paged(const gr_attn_paged_params* p, void* workspace, siz
  *     y  = c > 0 ? (x > 0 ? x / repetition[b] : x * repetition[b]) - (frequency[b] * c + presence[b]) : x
  *     y += bias[b, v]
  *     y  = -inf where the mask row of the beam has bit v clear, whatever x was
- * in fp32.  Rows of dead beams are left as they are.  `out` is `logits` itself (in place; rows without a bias or a mask are then changed at the counted
+ * in fp32.  Rows of dead beams are left as they are (in a new tensor: as the memory was; gr_beam_select does not look at them).  `out` is `logits` itself (in place; rows without a bias or a mask are then changed at the counted
  * tokens alone) or does not overlap it.  Any of the parts may be absent (NULL).  repetition is positive.  History rows whose
  * token lies outside [0, V) count nothing.
  * Supported: 1 <= V <= 32768; depth <= 8; n_history < 2^28.  Only enqueues on `stream`.  Errors: INVALID_ARG, UNSUPPORTED, HIP.
