@@ -347,8 +347,8 @@ gr_status gr_page_write(const gr_page_write_params* p, void* stream);
 /* gr_beam_attn_paged - gr_beam_attn over a prompt cache in pages.  The keys of beam w of request b are, in this order, the prefix_L tokens that all
  * requests share (pages prefix_pages[0], prefix_pages[1], ...), the request's own seq_lens[b] tokens (pages block_table[b, 0], ...), and
  * the beam's own u tokens, as for gr_beam_attn (with `slot` as for gr_beam_attn_slots, or NULL).  Any part may be empty; a beam
- * without a single key gets out = 0 and lse = -inf.  The prefix is read and multiplied once for the rows of all requests where that is
- * less work than with each request's rows by themselves.
+ * without a single key gets out = 0 and lse = -inf.  Where a request has at most 80 rows of a KV head (W * Hq/Hkv) and the launch rule estimates that it pays, the
+ * prefix is read and multiplied once for the rows of all requests; with more, each request's rows meet it by themselves.
  * What a table holds beyond a request's pages is of no effect; a page number outside [0, n_pages) is read as page 0, and a length outside [0, max_L] as the
  * nearer end.  Slots of a page behind a request's last token may hold anything.
  * GR_KV_FP8: pools of E4M3 codes, scales applied as in gr_beam_attn_fp8kv.

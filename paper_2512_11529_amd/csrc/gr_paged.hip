@@ -7,7 +7,8 @@
 //   - Softmax partials (maximum, sum, O) of disjoint sets of keys join exactly, so the prefix may be met by other workgroups than the rest.  A workgroup's
 //     128 or 256 rows share their keys: the rows of one (request, KV head) pair share all of them (W * g rows), the rows of ALL requests
 //     share the prefix.  Where a request's rows leave most of a workgroup empty, part 0 of the launch packs all requests' rows against the prefix, as if they were
-//     the beams of one request, and part 1 takes each request's own pages; a second kernel joins the partials.  Else a row walks the whole list by itself.
+//     the beams of one request, and part 1 takes each request's own pages; a second kernel joins the partials.  Else, and with more than 80 rows of a pair
+//     always, a row walks the whole list by itself.
 //   - Where a request's rows of a KV head are few, 32 of them meet the keys in a workgroup whose wavefronts share out the keys and not the rows.
 #include "gr_attn_rows.hpp"
 
@@ -385,7 +386,7 @@ __global__ void __launch_bounds__(256) k_paged_join(JoinCtx c) {
 // The launch.  rows: of a workgroup of part 1 (32, 128, 256); ns: segments of the prefix in part 0 (0: there is none) and of the list in part 1; ks and find as in gr_beam_attn.
 struct PagedPlan { int rows, ns[2], ks; bool find; };
 
-// More than 80 rows of a (request, KV head) pair are launched as gr_beam_attn launches them.  For fewer, the cheapest of these is taken, by their estimated time in us: blocks of 32 rows or of 128
+// More than 80 rows of a (request, KV head) pair are launched as gr_beam_attn launches them, and never share a prefix: part 1 exists in blocks of 32 rows alone.  For fewer, the cheapest of these is taken, by their estimated time in us: blocks of 32 rows or of 128
 // over the whole list, or the prefix packed, each with 1 to 16 segments.  The estimate of a launch is `start`, and (the fourth root of the sum of the fourth powers: a little more than the longer) of
 //   - what its keys take at `rate`;
 //   - its workgroups' time: `few` + `few_step` for every 128 tokens (blocks of 32), `unit` + `tile1` for every 64 (128; two sets of wavefronts where there is at most one workgroup per CU:
