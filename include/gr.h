@@ -361,7 +361,7 @@ typedef struct {
   int32_t ND, u;                  /* own-token capacity of a beam, and valid own tokens                */
   int32_t page_size, max_pages, n_pages;
   int32_t prefix_L;               /* tokens of the shared prefix                                       */
-  int32_t max_L;                  /* host copy of max_b seq_lens[b]; at most max_pages * page_size     */
+  int32_t max_L;                  /* max_b seq_lens[b] or more; at most max_pages * page_size           */
   int32_t kv_type;                /* GR_KV_*: element type of the pools                                */
   float   sm_scale;               /* positive and finite                                               */
   float   k_scale, v_scale;       /* GR_KV_FP8: positive and finite                                    */
@@ -378,7 +378,9 @@ typedef struct {
   float*         lse_out;         /* fp32 [B, W, Hq] or NULL                                           */
 } gr_attn_paged_params;
 
-/* Bytes of workspace for these shapes; pointers, scales, u and ND are not looked at (0 is possible).  Host only. */
+/* Bytes of workspace for these shapes; pointers, scales, u and ND are not looked at (0 is possible).  Host only.  The number is of this max_L and prefix_L and no bound for
+ * smaller ones: a shorter list may be cut into more segments.  max_L may be larger than any of seq_lens, so a program with one workspace passes its
+ * largest with every call (the lengths themselves are read on the GPU), or asks again for each. */
 size_t gr_beam_attn_paged_workspace_bytes(const gr_attn_paged_params* p);
 gr_status gr_beam_attn_paged(const gr_attn_paged_params* p, void* workspace, size_t workspace_bytes, void* stream);
 

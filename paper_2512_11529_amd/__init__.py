@@ -387,7 +387,8 @@ def gr_page_write(k, v, slot, k_pages, v_pages, k_scale=1.0, v_scale=1.0, stream
 
 
 def attn_paged_workspace_bytes(B, W, Hq, Hkv, d, max_L, prefix_L=0, fp8=False, page_size=16) -> int:
-    """Workspace bytes of gr_beam_attn_paged (the same for pages of any size)."""
+    """Workspace bytes of gr_beam_attn_paged (the same for pages of any size) with this max_L and prefix_L; shorter ones may need more.  A call's max_L may be larger than its
+    lengths."""
     p = _paged_shapes(B, W, Hq, Hkv, d, max_L, prefix_L, fp8, page_size)
     return int(load_library().gr_beam_attn_paged_workspace_bytes(ctypes.byref(p)))
 
@@ -402,7 +403,7 @@ def gr_beam_attn_paged(q, k_pages, v_pages, block_table, seq_lens, k_unshared, v
                        v_scale=1.0, slot=None, out=None, lse_out=None, workspace=None, stream=None):
     """Beam attention over a prompt cache in pages.  q bf16 [B,W,Hq,d]; k/v_pages [n_pages,page_size,Hkv,d], bf16 or uint8 (E4M3 codes, value = code * scale);
     block_table int32 [B,max_pages]; seq_lens int32 [B]; k/v_unshared bf16 [B,W,ND,Hkv,d] (None: no own tokens, u = 0); `slot` as for gr_beam_attn_slots.
-    prefix_pages int32 [prefix_L/page_size]: pages of the tokens in front that all requests share.  max_L (of seq_lens) and prefix_L are host
+    prefix_pages int32 [prefix_L/page_size]: pages of the tokens in front that all requests share.  max_L (the largest of seq_lens, or more) and prefix_L are host
     integers.  Returns (out bf16 [B,W,Hq,d], lse fp32 [B,W,Hq] or None).  Enqueues on `stream` (default: current)."""
     native = _native or _marshal()
     if out is None:

@@ -184,3 +184,14 @@ def test_a_forced_plan_is_of_the_packed_cache_alone(gr):
         assert lib.gr_diag_attn_plan(0, 0) == 0
     assert forced[0] == free[0] > 0 and forced[1] != free[1]
     assert (gr.attn_paged_workspace_bytes(**shape), gr.attn_workspace_bytes(**shape)) == free
+
+
+def test_a_shorter_list_may_need_a_larger_workspace(gr):
+    """The size is of one max_L, as gr.h says: a program with one workspace keeps to one max_L."""
+    lib = gr.load_library()
+    shape = dict(B=32, W=8, Hq=8, Hkv=8, d=64, prefix_L=512)
+    sizes = {max_L: gr.attn_paged_workspace_bytes(**shape, max_L=max_L) for max_L in range(16, 4000, 16)}
+    shorter = max(sizes, key=lambda n: sizes[n])
+    longer = next(n for n in sizes if n > shorter and sizes[n] < sizes[shorter])
+    p = ATTN(**{**GOOD_ATTN, **shape, "max_L": shorter, "max_pages": 256})
+    assert lib.gr_beam_attn_paged(ctypes.byref(p), A, sizes[longer], None) == -3
