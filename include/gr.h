@@ -308,7 +308,7 @@ enum {
  *             behind the last token
  *   taken     {pages taken from the free list, requests with new tokens that were not served}
  * The same inputs give the same tables, so a host that knows the lengths can follow the free list without reading anything back.  Only enqueues on
- * `stream`.  The outputs must not overlap the inputs or each other.  Supported: B <= 4096; max_pages * page_size, n_pages * page_size and
+ * `stream`.  The outputs must not overlap the inputs or each other.  Supported: B <= 4096; max_pages * page_size and n_pages * page_size below 2^31,
  * total_new below 2^31 - 1024.  Errors: INVALID_ARG, UNSUPPORTED, HIP. */
 typedef struct {
   int32_t B, page_size;
