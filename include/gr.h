@@ -67,7 +67,7 @@ const char* gr_status_string(gr_status s);
  *
  * Supported: d in {64, 128}; Hq % Hkv == 0; 1 <= u <= ND; L_b >= 0 (L_b + u >= 1).  All bf16 tensors must be
  * 16-byte aligned (INVALID_ARG otherwise) and hold finite values.  Sums are fp32 and normalised at the end:
- * |v| * 2^8 * (L_b + u) has to stay below 2^128.  The probabilities, not their sum, are rounded to bf16 for the product with V (an error of at most 2^-9 of a
+ * |v| * 2^8 * (L_b + u) has to stay below 2^128.  The probabilities, not their sum, are rounded to bf16 for the product with V (an error of at most 2^-8 of a
  * token's share each, beside the rounding of `out`); so do all attention calls here.
  * ------------------------------------------------------------------------------------------------ */
 typedef struct {
