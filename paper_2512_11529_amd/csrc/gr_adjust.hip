@@ -23,7 +23,8 @@ constexpr int kMaxHistory = 1 << 28;     // (kSparseRows rows that all of them c
 constexpr int kFew = 256;                 // counted against each other
 constexpr int kList = 1024;
 constexpr int kBins = 4096;
-// History rows of a thread on their way at once: 32 x 128 rows of 4096 in place, 0-3000 history rows, 16.5 us with one, 11.3; 35 x 7 of 928 7.3, 5.6.
+// History rows of a thread on their way at once.  us at the first step (one live row a request) with one and with four: 32 requests of 1000-3000 history rows, 4096 tokens in place,
+// 16.5, 11.4; 35 of 364-1091, 928 tokens copied, 7.3, 5.6.
 constexpr int kAhead = 4;
 
 struct AdjustCtx {
@@ -174,8 +175,8 @@ struct Counted {
       }
       return;
     }
-    // the history once more for as many rows as have room in the bins together, or for each part of one row (4 x 2 rows of 32768, 20000 history rows: 73 us; through it three times for
-    // each part, to clear, count and read only what it touches, 241)
+    // the history once more for as many rows as have room in the bins together, or for each part of one row (4 requests of 6667-20000 history rows that all continue their one live
+    // row of 32768 tokens: 73 us, 131 with two live rows each; through it three times for each part, to clear, count and read only what it touches, 241)
     const int width = min(v1 - v0, kBins), together = min(kBins / width, R);
     for (int r0 = 0; r0 < rows; r0 += together) {
       if (!((s.live >> r0) & ((1u << together) - 1u))) continue;
@@ -258,7 +259,7 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(6
       partly = partly || (ok[u] != 15 && ok[u] != 0);
     }
     // (masks alone: four that are forbidden are written unread, four that are not left alone.  Where a wavefront has some of which part is forbidden, it reads and
-    // writes them whole; 8192 rows of 8192 under random masks take 119 us so, 121 where single logits are written)
+    // writes them whole; 8192 rows of 8192 under random masks, with penalties, take 116 us so, 2 more where single logits are written; the call that copies, adds a bias and masks 107)
     partly = MODE != MASK || __any(partly);
     if (partly) {
 #pragma unroll
@@ -341,8 +342,8 @@ extern "C" gr_status gr_logits_adjust(const gr_logits_adjust_params* p, void* st
   c.bias_stride = p->bias_rows == 1 ? 0 : p->V;
   c.logits = p->logits; c.out = p->out; c.scores = p->scores; c.prefix = p->prefix; c.history = p->history; c.cu_history = p->cu_history;
   c.repetition = p->repetition; c.frequency = p->frequency; c.presence = p->presence; c.bias = p->bias; c.allowed = p->allowed; c.allowed_row = p->allowed_row;
-  // a workgroup looks through its request's history, so a long row is one workgroup's where there are rows enough (1024 rows of 20000 tokens, 1300-4000 history rows each,
-  // 104 us with three workgroups to a row); not at the first step, where most rows are dead
+  // a workgroup looks through its request's history, so a long row is one workgroup's where there are rows enough (8 x 128 rows of 20000 tokens, 1333-4000 history rows a request,
+  // bias and masks: 48.1 us; 8 x 127 with three workgroups to a row 50.9); not at the first step, where most rows are dead
   c.tiles = count && p->step > 0 && rows >= 1024 ? 1 : (p->V + kTile - 1) / kTile;
   c.tile = ((p->V + c.tiles - 1) / c.tiles + 31) / 32 * 32;
   c.row_blocks = (unsigned)((p->W + kSparseRows - 1) / kSparseRows);

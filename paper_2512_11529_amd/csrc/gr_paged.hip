@@ -394,7 +394,10 @@ struct PagedPlan { int rows, ns[2], ks; bool find; };
 // and, where there are several segments, `join` and the partials written and read at 2.7 TB/s.  Fitted to 870 random calls of 1 to 128 requests of 10 to 16384 tokens with 1 to 80 rows,
 // 430 of them behind a prefix of 64 to 8192 tokens, each timed in up to 40 ways: the mean call takes 1.03 times the best of them, the worst 1.63, and 120 others 1.047 and 1.35 (packed wherever that saves half of the
 // blocks, with segments for about one or two workgroups per CU, 1.07 without a prefix and 1.14 with one; with the longer of the two times alone 16 requests of 1500-3000 tokens x 8 beams
-// took 49.0 us in one segment each, now 39.7 in two, 64 x 8 of 2 KV heads 46.6, 40.7).
+// took 49.0 us in one segment each, now 39.7 in two, 64 x 8 of 2 KV heads 46.6, 40.7).  One call in twenty takes more than 1.15 times its best: mostly lists of thousands of tokens and
+// ragged lengths of head size 64, left in one segment (53 requests of 972-4736 x 1 beam of 8 heads in FP8 79 us, 57 in eight; 28 of 642-7763 x 54 in bf16 92, 66 in three), a few long lists in
+// sixteen (6 of 2342 x 2, 16 and 4 heads of 128, 17.9, 13.8 in eight), and prefixes of 64-800 tokens packed, or not, the wrong way (58 requests of 604 x 24 behind 512, 8 heads of 64, 27.5,
+// 21.3 not packed).
 struct PagedCost { double start, few, few_step, few_per_cu, unit, tile1, tile2, shared, shared_tile, join, rate; };
 constexpr PagedCost kPagedCost[2][2] = {      // [head size 128][FP8]; rate in bytes a us
     {{3.3, 1.5, 1.2, 2.0, 2.0, 1.05, 0.95, 1.5, 0.7, 3.1, 8.0e6}, {3.3, 1.5, 1.4, 2.0, 2.0, 1.05, 0.95, 1.5, 0.8, 3.1, 4.0e6}},
