@@ -11,7 +11,7 @@
  *      bytes, the update of a slot table that the attention follows (gr_beam_slot_update, gr_beam_attn_slots).
  * Beside the step: the prefill that fills the shared cache (gr_prefill_attn), the step's attention over a shared
  * cache stored in FP8 (gr_beam_attn_fp8kv), a prompt cache in pages with a prefix that requests share (gr_page_map, gr_page_write,
- * gr_beam_attn_paged), penalties, biases and masks on the logits (gr_logits_adjust), an item step for callers that cannot allocate
+ * gr_page_append, gr_page_read, gr_beam_attn_paged), norms and rotation of queries and keys (gr_qk_norm_rope), penalties, biases and masks on the logits (gr_logits_adjust), an item step for callers that cannot allocate
  * (gr_beam_select_noalloc), and a few diagnostics used by the benchmark (gr_diag_*).
  *
  * Conventions for every entry point
@@ -26,7 +26,7 @@
  *     call and synchronises `stream` once to report table errors.
  *   - Return value: GR_OK or a negative gr_status.  Nothing is printed, thrown or aborted.
  *     Host-checkable argument errors are reported before anything is enqueued.
- *   - The calls around pages and logits (gr_page_*, gr_beam_attn_paged, gr_logits_adjust) report UNSUPPORTED for shapes whose launch would
+ *   - The calls around pages and logits (gr_page_*, gr_beam_attn_paged, gr_qk_norm_rope, gr_logits_adjust) report UNSUPPORTED for shapes whose launch would
  *     have 2^32 threads or more (from 2^24 rows of logits on, or 2^23 blocks of query rows and segments).
  *   - bf16 tensors are raw 16-bit patterns; all tensors are dense, row-major, in the stated shape.
  */
@@ -284,18 +284,59 @@ gr_status gr_beam_slot_update(int32_t B, int32_t W, int32_t ND, int32_t u, const
 gr_status gr_beam_attn_slots(const gr_attn_params* p, const int32_t* slot, void* workspace, size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------------------------------
+ * gr_qk_norm_rope - queries and keys of T rows on their way from a projection to attention: every head normed by itself and rotated by the row's position.
+ *     y = x * w / sqrt(mean(x^2) + eps)                                 (q_weight, k_weight; NULL: y = x)
+ *     y_a' = y_a cos - y_b sin,  y_b' = y_b cos + y_a sin               for i < rot / 2, (a, b) = (i, i + rot / 2), or with pairs = 1 (2 i, 2 i + 1)
+ * with cos = table[pos, i], sin = table[pos, rot / 2 + i]; elements from rot on are not rotated.  In fp32, rounded to bf16 once.  Rows lie any strides apart: parts of a fused
+ * projection's rows, and the beams' own caches (a row's KV heads at k_unshared + ((b * W + w) * ND + token) * Hkv * d: a stride of ND * Hkv * d).  Queries or keys may be absent (NULL
+ * with their output).  v, which is only moved to v_out beside the keys, is for such caches and may be absent too.  With rot > 0 rows whose position is outside [0, n_pos) are left as they
+ * were in all outputs.  q_out is q itself (same stride), or does not overlap any input; so is k_out with k; v_out overlaps nothing.
+ * Only enqueues on `stream`.  Supported: d a multiple of 16 up to 256; rot a multiple of 16 up to d (0: no rotation; pos and table are not looked at); Hq * d and Hkv * d at most
+ * 2^20; strides multiples of 8; T < 2^31.  All tensors but pos 16-byte aligned.  Errors: INVALID_ARG, UNSUPPORTED, HIP.
+ * ------------------------------------------------------------------------------------------------ */
+typedef struct {
+  int64_t T;                      /* rows                                                              */
+  int32_t Hq, Hkv, d;
+  int32_t rot;                    /* leading elements of a head that are rotated                       */
+  int32_t pairs;                  /* 0: element i with i + rot / 2; 1: element 2 i with 2 i + 1        */
+  int32_t n_pos;                  /* rows of table                                                     */
+  float   eps;                    /* at least 0                                                        */
+  int64_t q_stride, k_stride, v_stride;                 /* elements from a row to the next             */
+  int64_t q_out_stride, k_out_stride, v_out_stride;
+  const void*    q;               /* bf16, Hq * d elements a row, or NULL                              */
+  const void*    k;               /* bf16, Hkv * d elements a row, or NULL                             */
+  const void*    v;               /* bf16, Hkv * d elements a row, or NULL                             */
+  const float*   q_weight;        /* fp32 [d] or NULL                                                  */
+  const float*   k_weight;        /* fp32 [d] or NULL                                                  */
+  const float*   table;           /* fp32 [n_pos, rot]                                                 */
+  const int32_t* pos;             /* int32 [T]                                                         */
+  void*          q_out;           /* bf16                                                              */
+  void*          k_out;
+  void*          v_out;
+} gr_qk_norm_rope_params;
+gr_status gr_qk_norm_rope(const gr_qk_norm_rope_params* p, void* stream);
+
+/* ------------------------------------------------------------------------------------------------
  * A prompt cache in pages.  gr_beam_attn reads a prompt cache that is packed for one batch.  A server whose requests come and go keeps the
  * prompts in pages of a pool instead, and a prefix that all of them share (an instruction, a context) once:
  *   gr_page_map          pages are handed out of a free list for the new tokens of every request; block tables and slot map
  *   gr_page_write        K/V rows of new tokens (as prefill produced them) into their slots, in bf16 or as FP8 codes
+ *   gr_page_append       the same for keys that are not yet normed and rotated, and for pages in FP4
+ *   gr_page_read         rows of pages back into a packed cache
  *   gr_beam_attn_paged   the decode step's attention over such pages
  * A pool is [n_pages, page_size, Hkv, d] for K and the same for V; page_size is a power of two from 16 to 1024.  Slot s of a pool is
  * token s % page_size of page s / page_size.  Token t of request b lies in page block_table[b, t / page_size].
  * ------------------------------------------------------------------------------------------------ */
 enum {
   GR_KV_BF16 = 0,
-  GR_KV_FP8 = 1                   /* OCP FP8 E4M3 codes, uint8; the value of an element is code * scale, one scale per tensor */
+  GR_KV_FP8 = 1,                  /* OCP FP8 E4M3 codes, uint8; the value of an element is code * scale, one scale per tensor */
+  GR_KV_FP4 = 2                   /* OCP MXFP4: E2M1 codes, a power of two as the scale of every 32; gr_page_append, gr_page_read, gr_beam_attn_paged */
 };
+
+/* Pools of GR_KV_FP4 are uint8 [n_pages, Hkv, gr_kv_fp4_page_bytes(page_size, d)], d a multiple of 32.  For a page and KV head they hold page_size rows of d / 2 bytes, element
+ * 2 i of a token in the low half of byte i, and behind them page_size rows of d / 32 bytes: element e's value is its code's (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives)
+ * times 2^(s - 127) with s the byte of block e / 32.  Written are s from 7 to 252, and 255 for a block that an infinite value or NaN is in: all of it is NaN. */
+size_t gr_kv_fp4_page_bytes(int32_t page_size, int32_t d);       /* host only; 0 for sizes that are not supported */
 
 /* gr_page_map - request b has seq_lens[b] tokens in its pages and gets new_lens[b] more (negative lengths count as 0).  Where its last page is full
  * (or it has none) it gets fresh pages, free_pages[0], free_pages[1], ... in the order of the requests, which are written into its row of
@@ -344,6 +385,49 @@ typedef struct {
   void*          v_pages;
 } gr_page_write_params;
 gr_status gr_page_write(const gr_page_write_params* p, void* stream);
+
+/* gr_page_append - gr_page_write for the rows of a projection: the keys are normed and rotated on the way, as gr_qk_norm_rope does it (k_weight NULL: not normed; rot 0: not
+ * rotated), in fp32 and rounded once, to the pool's type.  Values go as they are.  Rows whose slot is outside [0, n_pages * page_size) or, with rot > 0, whose position is outside
+ * [0, n_pos) are not written; a slot that two rows have holds either's elements, in parts too.  GR_KV_FP8: codes as gr_page_write makes them (of rotated or normed keys the quotient
+ * may be one unit of fp32 off the division's).  GR_KV_FP4: a block's scale is the smallest power of two, from 2^-120 to 2^125, with |x| <= 7 * scale for its 32 values (no value is
+ * further off than half the distance of the codes around it); codes are the nearest, ties to even.  Only enqueues on `stream`.  The pools do not overlap k, v or each other.
+ * Supported: d a multiple of 16 (GR_KV_FP4: 32) up to 256; rot a multiple of 16 up to d; Hkv * d at most 2^20; the strides multiples of 8; T and n_pages * page_size below
+ * 2^31.  k, v, the pools, k_weight and table 16-byte aligned.  Errors: INVALID_ARG, UNSUPPORTED, HIP. */
+typedef struct {
+  int64_t T;                      /* rows                                                              */
+  int32_t Hkv, d, page_size, n_pages;
+  int32_t kv_type;                /* GR_KV_*: element type of the pools                                */
+  int32_t rot, pairs, n_pos;      /* as for gr_qk_norm_rope                                            */
+  float   eps;
+  float   k_scale, v_scale;       /* GR_KV_FP8: positive and finite                                    */
+  int64_t k_stride, v_stride;     /* elements from a row to the next, at least Hkv * d                 */
+  const void*    k;               /* bf16                                                              */
+  const void*    v;               /* bf16                                                              */
+  const int32_t* slot;            /* int32 [T]                                                         */
+  const int32_t* pos;             /* int32 [T]; may be NULL when rot == 0                              */
+  const float*   table;           /* fp32 [n_pos, rot]; may be NULL when rot == 0                      */
+  const float*   k_weight;        /* fp32 [d] or NULL                                                  */
+  void*          k_pages;         /* as gr_page_write's, or GR_KV_FP4's                                */
+  void*          v_pages;
+} gr_page_append_params;
+gr_status gr_page_append(const gr_page_append_params* p, void* stream);
+
+/* gr_page_read - the rows in the slots slot[t] of the pools as bf16 rows t of k and v (k_stride and v_stride elements apart), packed as gr_beam_attn and gr_prefill_attn take them.
+ * The value of a code (times its scale, in fp32) is rounded to bf16; of FP4 it is exact for the scales that are written.  Rows whose slot is outside [0, n_pages * page_size) are left
+ * as they were.  k and v do not overlap the pools or each other.  Only enqueues on `stream`.  Supported: as for gr_page_append.  Errors: INVALID_ARG, UNSUPPORTED, HIP. */
+typedef struct {
+  int64_t T;                      /* rows                                                              */
+  int32_t Hkv, d, page_size, n_pages;
+  int32_t kv_type;                /* GR_KV_*: element type of the pools                                */
+  float   k_scale, v_scale;       /* GR_KV_FP8: positive and finite                                    */
+  int64_t k_stride, v_stride;     /* elements from a row to the next, at least Hkv * d                 */
+  const void*    k_pages;
+  const void*    v_pages;
+  const int32_t* slot;            /* int32 [T]                                                         */
+  void*          k;               /* bf16                                                              */
+  void*          v;               /* bf16                                                              */
+} gr_page_read_params;
+gr_status gr_page_read(const gr_page_read_params* p, void* stream);
 
 /* gr_beam_attn_paged - gr_beam_attn over a prompt cache in pages.  The keys of beam w of request b are, in this order, the prefix_L tokens that all
  * requests share (pages prefix_pages[0], prefix_pages[1], ...), the request's own seq_lens[b] tokens (pages block_table[b, 0], ...), and

@@ -7,7 +7,10 @@ The calls have the names and meaning of the C ABI in include/gr.h:
     gr_beam_select       masked log-softmax + beam score accumulation + top-W selection
     gr_beam_reorder      in-place move of the surviving beams' own KV cache to their new slots
     gr_page_map          pages of a pool handed out for new tokens: block tables and slot map
+    gr_qk_norm_rope      queries and keys normed head by head and rotated by their positions
     gr_page_write        K/V rows of new tokens into their slots of the pools (bf16 or FP8 codes)
+    gr_page_append       the same with the keys normed and rotated on the way, and for pools in FP4
+    gr_page_read         rows of the pools back into packed bf16
     gr_beam_attn_paged   beam attention over a prompt cache in pages, behind a prefix that all requests share
     gr_logits_adjust     penalties for seen items, biases and masks on the logits of an item step
 
@@ -26,7 +29,8 @@ __all__ = ["load_library", "gr_beam_attn", "gr_beam_attn_fp8kv", "gr_prefill_att
            "gr_status_string",
            "attn_workspace_bytes", "select_workspace_bytes", "GrError", "GR_SELECT_FORCE_DENSE", "LIB_PATH",
            "gr_diag_stream_read", "gr_diag_mfma_loop", "gr_diag_attn_plan", "gr_diag_attn_paged_plan", "gr_diag_issue_loop", "gr_diag_issue_loop_lds", "gr_beam_attn_slots", "gr_beam_slot_update",
-           "gr_page_map", "gr_page_write", "gr_beam_attn_paged", "attn_paged_workspace_bytes", "gr_logits_adjust"]
+           "gr_page_map", "gr_page_write", "gr_beam_attn_paged", "attn_paged_workspace_bytes", "gr_logits_adjust",
+           "gr_qk_norm_rope", "gr_page_append", "gr_page_read", "kv_fp4_page_bytes"]
 
 LIB_PATH = _build.LIB_PATH
 GR_SELECT_FORCE_DENSE = 1
@@ -128,7 +132,9 @@ def load_library(path: str = None):
     lib.gr_diag_mfma_flops.argtypes = [ctypes.c_int32, ctypes.c_int32]
     lib.gr_beam_reorder.restype = ctypes.c_int32
     lib.gr_beam_reorder.argtypes = [ctypes.c_int32] * 6 + [ctypes.c_void_p] * 4
-    for name in ("gr_page_map", "gr_page_write", "gr_logits_adjust"):
+    lib.gr_kv_fp4_page_bytes.restype = ctypes.c_size_t
+    lib.gr_kv_fp4_page_bytes.argtypes = [ctypes.c_int32, ctypes.c_int32]
+    for name in ("gr_page_map", "gr_page_write", "gr_page_append", "gr_page_read", "gr_qk_norm_rope", "gr_logits_adjust"):
         getattr(lib, name).restype = ctypes.c_int32
         getattr(lib, name).argtypes = [ctypes.c_void_p, ctypes.c_void_p]
     lib.gr_beam_attn_paged.restype = ctypes.c_int32
@@ -155,7 +161,8 @@ def _marshal():
         native.bind(*(ctypes.cast(getattr(lib, f), ctypes.c_void_p).value for f in (
             "gr_beam_attn", "gr_beam_attn_slots", "gr_beam_attn_fp8kv", "gr_beam_attn_workspace_bytes", "gr_prefill_attn", "gr_beam_select",
             "gr_beam_select_noalloc", "gr_beam_select_workspace_bytes", "gr_beam_reorder", "gr_beam_slot_update",
-            "gr_page_map", "gr_page_write", "gr_beam_attn_paged", "gr_beam_attn_paged_workspace_bytes", "gr_logits_adjust")), _current_stream_handle)
+            "gr_page_map", "gr_page_write", "gr_beam_attn_paged", "gr_beam_attn_paged_workspace_bytes", "gr_logits_adjust", "gr_qk_norm_rope", "gr_page_append",
+            "gr_page_read")), _current_stream_handle)
         _native = native
     return _native
 
@@ -384,6 +391,45 @@ def gr_page_write(k, v, slot, k_pages, v_pages, k_scale=1.0, v_scale=1.0, stream
     rc = (_native or _marshal()).page_write(k, v, slot, k_pages, v_pages, k_scale, v_scale, stream)
     if rc != 0:
         raise GrError(rc, "gr_page_write")
+
+
+def gr_qk_norm_rope(q, k, pos=None, table=None, q_weight=None, k_weight=None, eps=1e-6, pairs=False, q_out=None, k_out=None, v=None, v_out=None, stream=None):
+    """Queries and keys normed head by head and rotated.  q bf16 [T,Hq,d], k bf16 [T,Hkv,d] (either may be None): rows contiguous and any stride apart, as are q_out and k_out (new
+    tensors where they are None; the inputs themselves: in place).  q_weight, k_weight fp32 [d]: the norms' weights (None: not normed).  table fp32 [n_pos,rot]: rot/2 cosines, then
+    rot/2 sines of every position (None: not rotated), pos int32 [T]; rows whose position is outside the table are left as they were.  pairs: element 2i turns with 2i+1 instead of
+    i with i + rot/2.  v, v_out [T,Hkv,d]: values that are moved beside the keys.  Returns (q_out, k_out).  Enqueues on `stream`."""
+    native = _native or _marshal()
+    if q_out is None and q is not None:
+        q_out = _empty(q.shape, "bfloat16", q.device, stream)
+    if k_out is None and k is not None:
+        k_out = _empty(k.shape, "bfloat16", k.device, stream)
+    rc = native.norm_rope(q, k, v, pos, table, q_weight, k_weight, eps, pairs, q_out, k_out, v_out, stream)
+    if rc != 0:
+        raise GrError(rc, "gr_qk_norm_rope")
+    return q_out, k_out
+
+
+def kv_fp4_page_bytes(page_size, d) -> int:
+    """Bytes of a page and KV head of a pool in FP4, which is uint8 [n_pages, Hkv, kv_fp4_page_bytes(page_size, d)]; 0 for sizes that are not supported."""
+    return int(load_library().gr_kv_fp4_page_bytes(int(page_size), int(d)))
+
+
+def gr_page_append(k, v, slot, k_pages, v_pages, pos=None, table=None, k_weight=None, eps=1e-6, pairs=False, k_scale=1.0, v_scale=1.0, stream=None):
+    """K/V rows into their slots, the keys normed (k_weight) and rotated (pos, table, pairs) as by gr_qk_norm_rope on the way.  k, v, slot as for gr_page_write; k_pages, v_pages
+    [n_pages,page_size,Hkv,d] in bf16 or uint8 (E4M3 codes of x / scale), or uint8 [n_pages,Hkv,kv_fp4_page_bytes(page_size,d)] for FP4.  Rows whose slot is outside the pool or whose
+    position is outside the table are not written.  Enqueues on `stream`."""
+    rc = (_native or _marshal()).page_append(k, v, slot, k_pages, v_pages, pos, table, k_weight, eps, pairs, k_scale, v_scale, stream)
+    if rc != 0:
+        raise GrError(rc, "gr_page_append")
+
+
+def gr_page_read(k_pages, v_pages, slot, k, v, k_scale=1.0, v_scale=1.0, stream=None):
+    """The rows in slots `slot` int32 [T] of pools of any type into k, v bf16 [T,Hkv,d] (rows contiguous and any stride apart); rows whose slot is outside the pool are left as they
+    were.  Returns (k, v).  Enqueues on `stream`."""
+    rc = (_native or _marshal()).page_read(k_pages, v_pages, slot, k, v, k_scale, v_scale, stream)
+    if rc != 0:
+        raise GrError(rc, "gr_page_read")
+    return k, v
 
 
 def attn_paged_workspace_bytes(B, W, Hq, Hkv, d, max_L, prefix_L=0, fp8=False, page_size=16) -> int:

@@ -29,6 +29,9 @@ decltype(&gr_page_write) p_page_write = nullptr;
 decltype(&gr_beam_attn_paged) p_attn_paged = nullptr;
 decltype(&gr_beam_attn_paged_workspace_bytes) p_attn_paged_ws = nullptr;
 decltype(&gr_logits_adjust) p_adjust = nullptr;
+decltype(&gr_qk_norm_rope) p_norm_rope = nullptr;
+decltype(&gr_page_append) p_page_append = nullptr;
+decltype(&gr_page_read) p_page_read = nullptr;
 
 struct Error {};        // a Python exception is set
 
@@ -367,6 +370,144 @@ PyObject* page_write(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// A pool of any type for heads of size d: uint8 [n_pages, Hkv, bytes] is FP4, uint8 [n_pages, page_size, Hkv, d] FP8, bf16 of that shape bf16.
+struct Pool {
+  int32_t kv_type;
+  int64_t pages, page, Hkv;
+  at::ScalarType type;
+  const at::Tensor* t;
+};
+Pool any_pool(PyObject* o, const char* name, int64_t d) {
+  const at::Tensor* t = THPVariable_Check(o) ? &THPVariable_Unpack(o) : nullptr;
+  if (!(t && t->scalar_type() == at::kByte && t->dim() == 3)) {
+    bool fp8;
+    t = &pool(o, name, &fp8);
+    return {fp8 ? GR_KV_FP8 : GR_KV_BF16, t->size(0), t->size(1), t->size(2), fp8 ? at::kByte : at::kBFloat16, t};
+  }
+  t = &tensor_nd(o, at::kByte, name, 3);
+  const int64_t bytes = t->size(2), page = d > 0 && d % 32 == 0 ? bytes / (d / 2 + d / 32) : 0;
+  if (page == 0 || page * (d / 2 + d / 32) != bytes) {
+    PyErr_Format(PyExc_ValueError, "%s: expected pages of %lld bytes a token and KV head (head size %lld in FP4), got shape %s", name, (long long)(d / 2 + d / 32), (long long)d,
+                 shape_text(t->sizes()).c_str());
+    throw Error();
+  }
+  return {GR_KV_FP4, t->size(0), page, t->size(1), at::kByte, t};
+}
+// Optional tensors, each on the call's GPU
+void* given_on(OnDevice& on, PyObject* o, at::ScalarType type, const char* name, c10::IntArrayRef shape) {
+  if (o == Py_None) return nullptr;
+  const at::Tensor& t = tensor(o, type, name, shape);
+  on.add(name, t);
+  return t.data_ptr();
+}
+bool truth(PyObject* o) {
+  const int v = PyObject_IsTrue(o);
+  if (v < 0) throw Error();
+  return v != 0;
+}
+// Rows [T, heads, d] of the shape, or None (with their stride)
+void* rows_given(OnDevice& on, PyObject* o, const char* name, c10::IntArrayRef shape, int64_t* stride) {
+  *stride = 0;
+  if (o == Py_None) return nullptr;
+  const at::Tensor* t;
+  *stride = rows_of(o, name, &t);
+  if (t->sizes() != shape) {
+    PyErr_Format(PyExc_ValueError, "%s: expected shape %s, got %s", name, shape_text(shape).c_str(), shape_text(t->sizes()).c_str());
+    throw Error();
+  }
+  on.add(name, *t);
+  return t->data_ptr();
+}
+
+// norm_rope(q | None, k | None, v | None, pos | None, table | None, q_weight | None, k_weight | None, eps, pairs, q_out | None, k_out | None, v_out | None, stream) -> status
+PyObject* norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    count(n, 13);
+    OnDevice on;
+    const at::Tensor *q = nullptr, *k = nullptr;
+    if (a[0] != Py_None) rows_of(a[0], "q", &q);
+    if (a[1] != Py_None) rows_of(a[1], "k", &k);
+    if (!q && !k) { PyErr_SetString(PyExc_TypeError, "q or k: expected a CUDA tensor"); throw Error(); }
+    const at::Tensor& x = q ? *q : *k;
+    const int64_t T = x.size(0), d = x.size(2), Hq = q ? q->size(1) : 0, Hkv = k ? k->size(1) : a[2] != Py_None && THPVariable_Check(a[2]) && THPVariable_Unpack(a[2]).dim() == 3 ? THPVariable_Unpack(a[2]).size(1) : 0;
+    gr_qk_norm_rope_params p{};
+    p.q = rows_given(on, a[0], "q", {T, Hq, d}, &p.q_stride);
+    p.k = rows_given(on, a[1], "k", {T, Hkv, d}, &p.k_stride);
+    p.v = rows_given(on, a[2], "v", {T, Hkv, d}, &p.v_stride);
+    p.q_out = rows_given(on, a[9], "q_out", {T, Hq, d}, &p.q_out_stride);
+    p.k_out = rows_given(on, a[10], "k_out", {T, Hkv, d}, &p.k_out_stride);
+    p.v_out = rows_given(on, a[11], "v_out", {T, Hkv, d}, &p.v_out_stride);
+    p.pos = (const int32_t*)given_on(on, a[3], at::kInt, "pos", {T});
+    if (a[4] != Py_None) {
+      const at::Tensor& table = tensor_nd(a[4], at::kFloat, "table", 2);
+      p.n_pos = int32_of(table.size(0), "table");
+      p.rot = int32_of(table.size(1), "table");
+      p.table = (const float*)given_on(on, a[4], at::kFloat, "table", table.sizes());
+    }
+    p.q_weight = (const float*)given_on(on, a[5], at::kFloat, "q_weight", {d});
+    p.k_weight = (const float*)given_on(on, a[6], at::kFloat, "k_weight", {d});
+    p.T = T; p.Hq = int32_of(Hq, "q"); p.Hkv = int32_of(Hkv, "k"); p.d = int32_of(d, "q"); p.eps = (float)real(a[7]); p.pairs = truth(a[8]);
+    void* stream = on.stream(a[12]);
+    return status_of([&] { return p_norm_rope(&p, stream); });
+  });
+}
+
+// page_append(k, v, slot, k_pages, v_pages, pos | None, table | None, k_weight | None, eps, pairs, k_scale, v_scale, stream) -> status
+PyObject* page_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    count(n, 13);
+    OnDevice on;
+    const at::Tensor* k;
+    rows_of(a[0], "k", &k);
+    const int64_t T = k->size(0), Hkv = k->size(1), d = k->size(2);
+    gr_page_append_params p{};
+    p.k = rows_given(on, a[0], "k", {T, Hkv, d}, &p.k_stride);
+    p.v = rows_given(on, a[1], "v", {T, Hkv, d}, &p.v_stride);
+    const Pool kp = any_pool(a[3], "k_pages", d);
+    if (kp.kv_type == GR_KV_FP4) tensor(a[3], kp.type, "k_pages", {kp.pages, Hkv, kp.t->size(2)});
+    else tensor(a[3], kp.type, "k_pages", {kp.pages, kp.page, Hkv, d});
+    p.k_pages = given_on(on, a[3], kp.type, "k_pages", kp.t->sizes());
+    p.v_pages = given_on(on, a[4], kp.type, "v_pages", kp.t->sizes());
+    p.slot = (const int32_t*)given_on(on, a[2], at::kInt, "slot", {T});
+    p.pos = (const int32_t*)given_on(on, a[5], at::kInt, "pos", {T});
+    if (a[6] != Py_None) {
+      const at::Tensor& table = tensor_nd(a[6], at::kFloat, "table", 2);
+      p.n_pos = int32_of(table.size(0), "table");
+      p.rot = int32_of(table.size(1), "table");
+      p.table = (const float*)given_on(on, a[6], at::kFloat, "table", table.sizes());
+    }
+    p.k_weight = (const float*)given_on(on, a[7], at::kFloat, "k_weight", {d});
+    p.T = T; p.Hkv = int32_of(Hkv, "k"); p.d = int32_of(d, "k"); p.page_size = int32_of(kp.page, "k_pages"); p.n_pages = int32_of(kp.pages, "k_pages"); p.kv_type = kp.kv_type;
+    p.eps = (float)real(a[8]); p.pairs = truth(a[9]); p.k_scale = (float)real(a[10]); p.v_scale = (float)real(a[11]);
+    void* stream = on.stream(a[12]);
+    return status_of([&] { return p_page_append(&p, stream); });
+  });
+}
+
+// page_read(k_pages, v_pages, slot, k, v, k_scale, v_scale, stream) -> status
+PyObject* page_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    count(n, 8);
+    OnDevice on;
+    const at::Tensor* k;
+    rows_of(a[3], "k", &k);
+    const int64_t T = k->size(0), Hkv = k->size(1), d = k->size(2);
+    gr_page_read_params p{};
+    p.k = rows_given(on, a[3], "k", {T, Hkv, d}, &p.k_stride);
+    p.v = rows_given(on, a[4], "v", {T, Hkv, d}, &p.v_stride);
+    const Pool kp = any_pool(a[0], "k_pages", d);
+    if (kp.kv_type == GR_KV_FP4) tensor(a[0], kp.type, "k_pages", {kp.pages, Hkv, kp.t->size(2)});
+    else tensor(a[0], kp.type, "k_pages", {kp.pages, kp.page, Hkv, d});
+    p.k_pages = given_on(on, a[0], kp.type, "k_pages", kp.t->sizes());
+    p.v_pages = given_on(on, a[1], kp.type, "v_pages", kp.t->sizes());
+    p.slot = (const int32_t*)given_on(on, a[2], at::kInt, "slot", {T});
+    p.T = T; p.Hkv = int32_of(Hkv, "k"); p.d = int32_of(d, "k"); p.page_size = int32_of(kp.page, "k_pages"); p.n_pages = int32_of(kp.pages, "k_pages"); p.kv_type = kp.kv_type;
+    p.k_scale = (float)real(a[5]); p.v_scale = (float)real(a[6]);
+    void* stream = on.stream(a[7]);
+    return status_of([&] { return p_page_read(&p, stream); });
+  });
+}
+
 // attn_paged(q, k_pages, v_pages, block_table, seq_lens, k_own | None, v_own | None, u, sm_scale, max_L, prefix_pages | None, prefix_L, k_scale, v_scale,
 //            slot | None, out, lse | None, workspace | None, stream) -> status (<= 0), or the workspace bytes that the call needs when none was given
 PyObject* attn_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
@@ -382,13 +523,12 @@ PyObject* attn_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
       on.add(name, t);
       return t.data_ptr();
     };
-    bool fp8;
-    const at::Tensor& kp = pool(a[1], "k_pages", &fp8);
-    const at::ScalarType type = fp8 ? at::kByte : at::kBFloat16;
-    const int64_t pages = kp.size(0), page = kp.size(1), Hkv = kp.size(2);
+    const Pool kp = any_pool(a[1], "k_pages", d);
+    const int64_t pages = kp.pages, page = kp.page, Hkv = kp.Hkv;
+    if (kp.kv_type != GR_KV_FP4) tensor(a[1], kp.type, "k_pages", {pages, page, Hkv, d});
     gr_attn_paged_params p{};
-    p.k_pages = given(a[1], type, "k_pages", {pages, page, Hkv, d});
-    p.v_pages = given(a[2], type, "v_pages", {pages, page, Hkv, d});
+    p.k_pages = given(a[1], kp.type, "k_pages", kp.t->sizes());
+    p.v_pages = given(a[2], kp.type, "v_pages", kp.t->sizes());
     const at::Tensor& table = tensor_nd(a[3], at::kInt, "block_table", 2);
     p.block_table = (const int32_t*)given(a[3], at::kInt, "block_table", {B, table.size(1)});
     p.seq_lens = (const int32_t*)given(a[4], at::kInt, "seq_lens", {B});
@@ -403,7 +543,7 @@ PyObject* attn_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
     p.lse_out = (float*)given(a[16], at::kFloat, "lse_out", {B, W, Hq});
     p.B = (int32_t)B; p.W = (int32_t)W; p.Hq = (int32_t)Hq; p.Hkv = (int32_t)Hkv; p.d = (int32_t)d; p.ND = (int32_t)ND; p.u = int32_of(integer(a[7]), "u");
     p.page_size = (int32_t)page; p.max_pages = int32_of(table.size(1), "block_table"); p.n_pages = (int32_t)pages; p.prefix_L = (int32_t)prefix_L; p.max_L = (int32_t)max_L;
-    p.kv_type = fp8 ? GR_KV_FP8 : GR_KV_BF16;
+    p.kv_type = kp.kv_type;
     p.sm_scale = (float)real(a[8]); p.k_scale = (float)real(a[12]); p.v_scale = (float)real(a[13]);
     p.q = q.data_ptr();
     size_t ws_bytes;
@@ -458,10 +598,10 @@ PyObject* adjust(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// bind(addresses of the fifteen entry points in the order of their declaration above, callable that returns the current stream's handle)
+// bind(addresses of the eighteen entry points in the order of their declaration above, callable that returns the current stream's handle)
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded([&]() -> PyObject* {
-    count(n, 16);
+    count(n, 19);
     p_attn = (decltype(p_attn))pointer(a[0]);
     p_attn_slots = (decltype(p_attn_slots))pointer(a[1]);
     p_attn_fp8kv = (decltype(p_attn_fp8kv))pointer(a[2]);
@@ -477,8 +617,11 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
     p_attn_paged = (decltype(p_attn_paged))pointer(a[12]);
     p_attn_paged_ws = (decltype(p_attn_paged_ws))pointer(a[13]);
     p_adjust = (decltype(p_adjust))pointer(a[14]);
-    Py_INCREF(a[15]);
-    Py_XSETREF(current_stream, a[15]);
+    p_norm_rope = (decltype(p_norm_rope))pointer(a[15]);
+    p_page_append = (decltype(p_page_append))pointer(a[16]);
+    p_page_read = (decltype(p_page_read))pointer(a[17]);
+    Py_INCREF(a[18]);
+    Py_XSETREF(current_stream, a[18]);
     Py_RETURN_NONE;
   });
 }
@@ -491,6 +634,9 @@ PyMethodDef methods[] = {{"attn", (PyCFunction)(void*)attn, METH_FASTCALL, nullp
                          {"page_map", (PyCFunction)(void*)page_map, METH_FASTCALL, nullptr},
                          {"page_write", (PyCFunction)(void*)page_write, METH_FASTCALL, nullptr},
                          {"attn_paged", (PyCFunction)(void*)attn_paged, METH_FASTCALL, nullptr},
+                         {"norm_rope", (PyCFunction)(void*)norm_rope, METH_FASTCALL, nullptr},
+                         {"page_append", (PyCFunction)(void*)page_append, METH_FASTCALL, nullptr},
+                         {"page_read", (PyCFunction)(void*)page_read, METH_FASTCALL, nullptr},
                          {"adjust", (PyCFunction)(void*)adjust, METH_FASTCALL, nullptr},
                          {"bind", (PyCFunction)(void*)bind, METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};

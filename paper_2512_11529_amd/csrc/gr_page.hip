@@ -1,11 +1,12 @@
-// gr_page_map, gr_page_write: a prompt cache kept in pages of a pool.
+// gr_page_map, gr_page_write, gr_page_read: a prompt cache kept in pages of a pool.
 //
 // Request b has s_b tokens in its pages and gets n_b more.  With ps tokens to a page it needs
 //     need_b = ceil((s_b + n_b) / ps) - ceil(s_b / ps)
 // fresh pages; off_b, the sum of need over the requests before it, is where they begin in the list of free pages, and cu_b, the sum of n,
 // where its tokens begin among the new ones.  Both sums are of whole numbers in a fixed order, so the same lengths and the same free list
 // always give the same tables.
-#include "gr_internal.hpp"
+#include <type_traits>
+#include "gr_pages.hpp"
 
 namespace {
 
@@ -154,35 +155,13 @@ struct WriteCtx {
   void* v_pages;
 };
 
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-
 // Eight bf16 values as E4M3 codes of x / scale: the division in fp32 as IEEE has it, saturated, rounded to nearest even; NaN stays NaN.
-// FAST: the quotient from the scale's reciprocal r (rounded to nearest) and one correction by the exact remainder, q = q0 + (x - q0 scale) r with q0 = x r, which rounds as the
-// division does (Markstein's theorem; of the 2^30 pairs of a scale's significand and a bf16 value's none differs from the division.  Powers of two beside them change nothing
-// for scales from 2^-60 to 2^60, where the remainder of a value whose code is not 0 is far from underflow).
-// q0 is held within +-512, so that an infinite one does not make the remainder NaN: the result saturates all the same.  16 x 60-700 rows of 8 x 128 from a fused projection
-// 10.0 us with the division.
 template <bool FAST>
-__device__ __forceinline__ u32x2 codes8(u32x4 w, float scale, float r) {
+__device__ __forceinline__ kv_u32x2 codes8(kv_u32x4 w, float scale, float r) {
   float f[8];
 #pragma unroll
-  for (int i = 0; i < 8; i++) {
-    const float x = __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
-    float y;
-    if (FAST) {
-      const float q0 = fminf(fmaxf(x * r, -512.f), 512.f);
-      y = copysignf(fmaf(fmaf(-q0, scale, x), r, q0), x);        // (-0 lost its sign)
-    } else {
-      y = x / scale;
-    }
-    f[i] = x != x ? x : fminf(fmaxf(y, -448.f), 448.f);
-  }
-  int a = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], 0, false);
-  a = __builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], a, true);
-  int b = __builtin_amdgcn_cvt_pk_fp8_f32(f[4], f[5], 0, false);
-  b = __builtin_amdgcn_cvt_pk_fp8_f32(f[6], f[7], b, true);
-  return u32x2{(uint32_t)a, (uint32_t)b};
+  for (int i = 0; i < 8; i++) f[i] = fp8_quotient<FAST>(bf16_at(w[i / 2], i & 1), scale, r);
+  return kv_u32x2{fp8_codes4(f[0], f[1], f[2], f[3]), fp8_codes4(f[4], f[5], f[6], f[7])};
 }
 
 // Bound: memory, 4 bytes an element in and out (FP8: 3).  A thread moves U pieces of 16 bytes of K and of V; all its rows are on their way before the
@@ -191,7 +170,7 @@ template <int FP8, int U>      // FP8: 0 bf16, 1 codes by the corrected reciproc
 __global__ void __launch_bounds__(256) k_page_write(WriteCtx c) {
   const uint32_t row0 = blockIdx.x * c.rows_wg, n = min(c.rows_wg, c.T - row0) * c.pieces;
   for (uint32_t i0 = threadIdx.x; i0 < n; i0 += 256 * U) {
-    u32x4 kx[U], vx[U];
+    kv_u32x4 kx[U], vx[U];
     int to[U];
     uint32_t piece[U];
 #pragma unroll
@@ -200,26 +179,102 @@ __global__ void __launch_bounds__(256) k_page_write(WriteCtx c) {
       const size_t row = row0 + r;
       piece[u] = i - r * c.pieces;
       to[u] = i0 + 256 * u < n ? c.slot[row] : -1;
-      kx[u] = *(const u32x4*)(c.k + (int64_t)row * c.k_stride + piece[u] * 8);
-      vx[u] = *(const u32x4*)(c.v + (int64_t)row * c.v_stride + piece[u] * 8);
+      kx[u] = *(const kv_u32x4*)(c.k + (int64_t)row * c.k_stride + piece[u] * 8);
+      vx[u] = *(const kv_u32x4*)(c.v + (int64_t)row * c.v_stride + piece[u] * 8);
     }
 #pragma unroll
     for (int u = 0; u < U; u++) {
       if ((uint32_t)to[u] >= c.n_slots) continue;
       const size_t at = (size_t)(uint32_t)to[u] * c.pieces + piece[u];
       if (FP8) {
-        ((u32x2*)c.k_pages)[at] = codes8<FP8 == 1>(kx[u], c.k_scale, c.k_rcp);
-        ((u32x2*)c.v_pages)[at] = codes8<FP8 == 1>(vx[u], c.v_scale, c.v_rcp);
+        ((kv_u32x2*)c.k_pages)[at] = codes8<FP8 == 1>(kx[u], c.k_scale, c.k_rcp);
+        ((kv_u32x2*)c.v_pages)[at] = codes8<FP8 == 1>(vx[u], c.v_scale, c.v_rcp);
       } else {
-        ((u32x4*)c.k_pages)[at] = kx[u];
-        ((u32x4*)c.v_pages)[at] = vx[u];
+        ((kv_u32x4*)c.k_pages)[at] = kx[u];
+        ((kv_u32x4*)c.v_pages)[at] = vx[u];
       }
     }
   }
 }
 
-bool page_size_ok(int32_t ps) { return ps >= 16 && ps <= 1024 && (ps & (ps - 1)) == 0; }
-bool scale_ok(float s) { return s > 0.f && s < INFINITY; }
+// ------------------------------------------------------------------------------------------------ read
+struct ReadCtx {
+  uint32_t T, chunks, inv_chunks;      // rows; workgroups of a row's heads
+  int Hkv, d, shift;
+  uint32_t n_slots;
+  int64_t k_stride, v_stride;
+  float k_scale, v_scale;
+  const uint8_t* k_pages;
+  const uint8_t* v_pages;
+  const int32_t* slot;
+  uint16_t* k;
+  uint16_t* v;
+};
+
+// Bound: memory, 4 bytes an element in and out (FP8 3, FP4 2.5).  A lane takes 16 consecutive elements of a head, a wavefront the same head of 64 / LG consecutive rows: of
+// FP4 pages, whose tokens of a head lie together, it reads runs of codes and of scales.
+template <int LG, int KV, int U>
+__global__ void __launch_bounds__(256) k_page_read(ReadCtx c) {
+  uint32_t group = __umulhi(blockIdx.x, c.inv_chunks);
+  group += blockIdx.x - group * c.chunks >= c.chunks ? 1u : 0u;
+  const uint32_t chunk = blockIdx.x - group * c.chunks;
+  const int lane = (int)threadIdx.x & 63, heads = 2 * c.Hkv;
+  const uint32_t row = group * (64 / LG) + (uint32_t)(lane / LG), e0 = (uint32_t)(lane % LG) * 16, d = (uint32_t)c.d;
+  if (row >= c.T || e0 >= d) return;
+  const uint32_t slot = (uint32_t)c.slot[row];
+  if (slot >= c.n_slots) return;
+  const int h0 = ((int)chunk * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6)) * U;
+  kv_u32x4 x[U][KV == GR_KV_BF16 ? 2 : 1];
+  uint32_t power[U];
+#pragma unroll
+  for (int u = 0; u < U; u++) {
+    const int h = min(h0 + u, heads - 1);
+    const bool is_k = h < c.Hkv;
+    const unsigned hk = (unsigned)(is_k ? h : h - c.Hkv);
+    const uint8_t* pages = is_k ? c.k_pages : c.v_pages;
+    if (KV == GR_KV_FP4) {
+      const uint32_t ps = 1u << c.shift, tok = slot & (ps - 1);
+      const uint8_t* record = pages + ((size_t)(slot >> c.shift) * (unsigned)c.Hkv + hk) * gr_fp4_record(ps, d);
+      const kv_u32x2 w = *(const kv_u32x2*)(record + tok * (d / 2) + e0 / 2);
+      x[u][0] = kv_u32x4{w[0], w[1], 0, 0};
+      power[u] = record[gr_fp4_codes(ps, d) + tok * (d / 32) + e0 / 32];
+    } else {
+      const size_t i = ((size_t)slot * (unsigned)c.Hkv + hk) * d + e0;
+      if (KV == GR_KV_FP8) {
+        x[u][0] = *(const kv_u32x4*)(pages + i);
+      } else {
+        const kv_u32x4* from = (const kv_u32x4*)((const uint16_t*)pages + i);
+        x[u][0] = from[0];
+        x[u][KV == GR_KV_BF16 ? 1 : 0] = from[1];
+      }
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < U; u++) {
+    const int h = h0 + u;
+    if (h >= heads) return;
+    const bool is_k = h < c.Hkv;
+    kv_u32x4* to = (kv_u32x4*)(is_k ? c.k + (int64_t)row * c.k_stride + h * c.d + e0 : c.v + (int64_t)row * c.v_stride + (h - c.Hkv) * c.d + e0);
+    kv_u32x4 y[2];
+    if (KV == GR_KV_BF16) {
+      y[0] = x[u][0]; y[1] = x[u][KV == GR_KV_BF16 ? 1 : 0];
+    } else if (KV == GR_KV_FP8) {
+      const float scale = is_k ? c.k_scale : c.v_scale;
+#pragma unroll
+      for (int i = 0; i < 4; i++) {
+        const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)x[u][0][i], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)x[u][0][i], true);
+        y[i / 2][2 * (i % 2)] = bf16_pair(lo[0] * scale, lo[1] * scale);
+        y[i / 2][2 * (i % 2) + 1] = bf16_pair(hi[0] * scale, hi[1] * scale);
+      }
+    } else {                           // exact: two bits of significand and a power of two
+#pragma unroll
+      for (int p = 0; p < 2; p++) y[p] = fp4_values8(x[u][0][p], power[u]);
+      if (power[u] == 255u) y[0] = y[1] = kv_u32x4{0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};
+    }
+    to[0] = y[0];
+    to[1] = y[1];
+  }
+}
 
 }  // namespace
 
@@ -232,7 +287,7 @@ extern "C" gr_status gr_page_map(const gr_page_map_params* p, void* stream_) {
   if (((uintptr_t)p->seq_lens | (uintptr_t)p->new_lens | (uintptr_t)p->free_pages | (uintptr_t)p->block_table | (uintptr_t)p->lens_out |
        (uintptr_t)p->cu_new | (uintptr_t)p->slot | (uintptr_t)p->taken) & 3)
     return GR_ERR_INVALID_ARG;
-  if (!page_size_ok(p->page_size) || p->B > kMapMaxB) return GR_ERR_UNSUPPORTED;
+  if (!gr_page_size_ok(p->page_size) || p->B > kMapMaxB) return GR_ERR_UNSUPPORTED;
   if (p->total_new >= ((int64_t)1 << 31) - 1024 || (int64_t)p->max_pages * p->page_size >= ((int64_t)1 << 31) ||
       (int64_t)p->n_pages * p->page_size >= ((int64_t)1 << 31))
     return GR_ERR_UNSUPPORTED;                                 // positions and slots are 32-bit numbers
@@ -253,13 +308,13 @@ extern "C" gr_status gr_page_write(const gr_page_write_params* p, void* stream_)
   if (p->T < 0 || p->Hkv <= 0 || p->d <= 0 || p->n_pages <= 0) return GR_ERR_INVALID_ARG;
   if (p->kv_type != GR_KV_BF16 && p->kv_type != GR_KV_FP8) return GR_ERR_INVALID_ARG;
   const bool fp8 = p->kv_type == GR_KV_FP8;
-  if (fp8 && (!scale_ok(p->k_scale) || !scale_ok(p->v_scale))) return GR_ERR_INVALID_ARG;
+  if (fp8 && (!gr_scale_ok(p->k_scale) || !gr_scale_ok(p->v_scale))) return GR_ERR_INVALID_ARG;
   const int64_t n = (int64_t)p->Hkv * p->d;
   if (!p->k_pages || !p->v_pages || p->k_pages == p->v_pages) return GR_ERR_INVALID_ARG;
   if (p->T > 0 && (!p->k || !p->v || !p->slot)) return GR_ERR_INVALID_ARG;
   if (p->k_stride < n || p->v_stride < n) return GR_ERR_INVALID_ARG;
   if (((uintptr_t)p->k | (uintptr_t)p->v | (uintptr_t)p->k_pages | (uintptr_t)p->v_pages) & 15 || ((uintptr_t)p->slot & 3)) return GR_ERR_INVALID_ARG;
-  if (!page_size_ok(p->page_size) || n % 8 || p->k_stride % 8 || p->v_stride % 8 || n > 1 << 20) return GR_ERR_UNSUPPORTED;
+  if (!gr_page_size_ok(p->page_size) || n % 8 || p->k_stride % 8 || p->v_stride % 8 || n > 1 << 20) return GR_ERR_UNSUPPORTED;
   if ((int64_t)p->n_pages * p->page_size >= ((int64_t)1 << 31) || p->T >= ((int64_t)1 << 31)) return GR_ERR_UNSUPPORTED;
   if (p->T == 0) return GR_OK;
   WriteCtx c;
@@ -278,6 +333,50 @@ extern "C" gr_status gr_page_write(const gr_page_write_params* p, void* stream_)
   if (u == 4) { if (type == 0) GR_LAUNCH(0, 4); else if (type == 1) GR_LAUNCH(1, 4); else GR_LAUNCH(2, 4); }
   else { if (type == 0) GR_LAUNCH(0, 1); else if (type == 1) GR_LAUNCH(1, 1); else GR_LAUNCH(2, 1); }
 #undef GR_LAUNCH
+  GR_HIP_TRY(hipGetLastError());
+  return GR_OK;
+}
+
+extern "C" size_t gr_kv_fp4_page_bytes(int32_t page_size, int32_t d) {
+  return gr_page_size_ok(page_size) && d > 0 && d % 32 == 0 && d <= 256 ? gr_fp4_record((uint32_t)page_size, (uint32_t)d) : 0;
+}
+
+extern "C" gr_status gr_page_read(const gr_page_read_params* p, void* stream_) {
+  if (!p) return GR_ERR_INVALID_ARG;
+  if (p->T < 0 || p->Hkv <= 0 || p->d <= 0 || p->n_pages <= 0) return GR_ERR_INVALID_ARG;
+  if (p->kv_type != GR_KV_BF16 && p->kv_type != GR_KV_FP8 && p->kv_type != GR_KV_FP4) return GR_ERR_INVALID_ARG;
+  if (p->kv_type == GR_KV_FP8 && (!gr_scale_ok(p->k_scale) || !gr_scale_ok(p->v_scale))) return GR_ERR_INVALID_ARG;
+  const int64_t n = (int64_t)p->Hkv * p->d;
+  if (!p->k_pages || !p->v_pages) return GR_ERR_INVALID_ARG;
+  if (p->T > 0 && (!p->k || !p->v || !p->slot || p->k == p->v)) return GR_ERR_INVALID_ARG;
+  if (p->k_stride < n || p->v_stride < n) return GR_ERR_INVALID_ARG;
+  if (((uintptr_t)p->k | (uintptr_t)p->v | (uintptr_t)p->k_pages | (uintptr_t)p->v_pages) & 15 || ((uintptr_t)p->slot & 3)) return GR_ERR_INVALID_ARG;
+  if (!gr_page_size_ok(p->page_size) || p->d % 16 || p->d > 256 || p->k_stride % 8 || p->v_stride % 8 || n > 1 << 20) return GR_ERR_UNSUPPORTED;
+  if (p->kv_type == GR_KV_FP4 && p->d % 32) return GR_ERR_UNSUPPORTED;
+  if ((int64_t)p->n_pages * p->page_size >= ((int64_t)1 << 31) || p->T >= ((int64_t)1 << 31)) return GR_ERR_UNSUPPORTED;
+  if (p->T == 0) return GR_OK;
+  ReadCtx c;
+  c.T = (uint32_t)p->T; c.Hkv = p->Hkv; c.d = p->d; c.shift = __builtin_ctz((unsigned)p->page_size); c.n_slots = (uint32_t)(p->n_pages * p->page_size);
+  c.k_stride = p->k_stride; c.v_stride = p->v_stride; c.k_scale = p->k_scale; c.v_scale = p->v_scale;
+  c.k_pages = (const uint8_t*)p->k_pages; c.v_pages = (const uint8_t*)p->v_pages; c.slot = p->slot; c.k = (uint16_t*)p->k; c.v = (uint16_t*)p->v;
+  auto go = [&](auto lanes, auto type) {
+    constexpr int LG = decltype(lanes)::value, KV = decltype(type)::value, U = 1;
+    c.chunks = (uint32_t)((2 * p->Hkv + 4 * U - 1) / (4 * U));
+    c.inv_chunks = 0xffffffffu / c.chunks;
+    const int64_t grid = (p->T + 64 / LG - 1) / (64 / LG) * c.chunks;
+    if (!gr_grid_fits(grid, 256)) return (gr_status)GR_ERR_UNSUPPORTED;
+    hipLaunchKernelGGL((k_page_read<LG, KV, U>), dim3((unsigned)grid), dim3(256), 0, (hipStream_t)stream_, c);
+    return (gr_status)GR_OK;
+  };
+  auto of_type = [&](auto lanes) {
+    return p->kv_type == GR_KV_BF16  ? go(lanes, std::integral_constant<int, GR_KV_BF16>())
+           : p->kv_type == GR_KV_FP8 ? go(lanes, std::integral_constant<int, GR_KV_FP8>())
+                                     : go(lanes, std::integral_constant<int, GR_KV_FP4>());
+  };
+  const gr_status st = p->d <= 64    ? of_type(std::integral_constant<int, 4>())
+                       : p->d <= 128 ? of_type(std::integral_constant<int, 8>())
+                                     : of_type(std::integral_constant<int, 16>());
+  if (st) return st;
   GR_HIP_TRY(hipGetLastError());
   return GR_OK;
 }

@@ -1,0 +1,424 @@
+// gr_qk_norm_rope, gr_page_append: what stands between a projection and attention.
+//
+// A head x of d elements is normed, y = x w / sqrt(mean(x^2) + eps), and its first `rot` elements are turned in pairs by the angles of the row's position,
+//     y_a' = y_a cos - y_b sin,   y_b' = y_b cos + y_a sin,
+// with (a, b) = (i, i + rot / 2) or (2 i, 2 i + 1) for i < rot / 2.  All of it is in fp32; the only rounding to fewer bits is the store's.
+//
+// Bound: memory, 4 bytes an element in and out (bf16).  A lane holds 16 consecutive elements of a head, 4, 8 or 16 lanes the head, and a wavefront the same head of
+// 16, 8 or 4 consecutive rows: what it writes into an FP4 page is then one run of codes and one of scales, whole 32-byte sectors, and a lane's cosines and sines serve
+// all of its heads.  The wavefronts of a workgroup take different heads of the same rows.  The other halves of pairs (i, i + rot / 2) are loaded a second time, from L1.
+#include <initializer_list>
+#include <type_traits>
+#include "gr_pages.hpp"
+
+namespace {
+
+__device__ __forceinline__ unsigned div_by(unsigned n, unsigned d, uint32_t inv) {      // inv = (2^32 - 1) / d, rounded down: the product's high word is n / d or one less
+  const unsigned q = __umulhi(n, inv);
+  return q + (n - q * d >= d ? 1u : 0u);
+}
+
+// Sum and maximum over groups of LG neighbouring lanes, in all of them.
+template <int CTRL>
+__device__ __forceinline__ float lanes_of(float v) {
+  return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, 0xf, 0xf, false));
+}
+template <int LG>
+__device__ __forceinline__ float group_sum(float v) {
+  v += lanes_of<0xb1>(v);                        // lane ^ 1
+  v += lanes_of<0x4e>(v);                        // lane ^ 2
+  if (LG >= 8) v += lanes_of<0x141>(v);          // the other four of eight (in reverse, but they are alike)
+  if (LG >= 16) v += lanes_of<0x140>(v);
+  return v;
+}
+
+struct TurnCtx {
+  uint32_t T, chunks, inv_chunks;      // rows; workgroups of a row's heads
+  int d, rot, n_pos;
+  float inv_d, eps;
+  const float* table;                  // [n_pos, rot]
+  const int32_t* pos;
+};
+
+// A wavefront's rows and a lane's part of them.
+template <int LG>
+struct Place {
+  uint32_t row, chunk;                 // (rows past the last one as that one)
+  int at, e0;                          // position; first of the lane's elements
+  bool live, holds;                    // the row is written; the head has these elements
+  __device__ __forceinline__ Place(const TurnCtx& c) {
+    const uint32_t group = div_by(blockIdx.x, c.chunks, c.inv_chunks);
+    const int lane = (int)threadIdx.x & 63;
+    chunk = blockIdx.x - group * c.chunks;
+    row = group * (64 / LG) + (uint32_t)(lane / LG);
+    live = row < c.T;
+    row = min(row, c.T - 1);
+    e0 = (lane % LG) * 16;
+    holds = e0 < c.d;
+    at = 0;
+    if (c.rot > 0) {
+      at = c.pos[row];
+      if ((unsigned)at >= (unsigned)c.n_pos) { live = false; at = 0; }
+    }
+    if (!holds) e0 = 0;                // (loads what the first lane does)
+  }
+};
+
+// Cosines and sines of a lane's 16 elements; of pairs (2 i, 2 i + 1) one for two.
+template <bool PAIRS>
+struct Angles {
+  float cs[PAIRS ? 8 : 16], sn[PAIRS ? 8 : 16];
+  int other[PAIRS ? 1 : 2];            // first of the elements that its two eights are paired with
+  bool turns;
+  __device__ __forceinline__ Angles(const TurnCtx& c, int at, int e0) {
+    turns = e0 < c.rot;
+    const int half = c.rot >> 1;
+    const float* t = c.table + (size_t)(unsigned)at * (unsigned)c.rot;
+    auto load8 = [](const float* p, float* to) {
+      const float4 a = *(const float4*)p, b = *(const float4*)(p + 4);
+      to[0] = a.x; to[1] = a.y; to[2] = a.z; to[3] = a.w; to[4] = b.x; to[5] = b.y; to[6] = b.z; to[7] = b.w;
+    };
+    if (PAIRS) {
+      if (turns) {
+        load8(t + (e0 >> 1), cs);
+        load8(t + half + (e0 >> 1), sn);
+      }
+      return;
+    }
+#pragma unroll
+    for (int p = 0; p < 2; p++) {      // (rot is a multiple of 16: eight elements are all in the same half)
+      const int e = e0 + 8 * p;
+      const bool low = e < half;
+      const int i = low ? e : e - half;
+      other[PAIRS ? 0 : p] = turns ? (low ? e + half : i) : e;
+      if (turns) {
+        load8(t + i, cs + (PAIRS ? 0 : 8 * p));
+        load8(t + half + i, sn + (PAIRS ? 0 : 8 * p));
+        if (low) {
+#pragma unroll
+          for (int k = 0; k < 8; k++) sn[PAIRS ? k : 8 * p + k] = -sn[PAIRS ? k : 8 * p + k];
+        }
+      }
+    }
+  }
+};
+
+template <bool PAIRS>
+struct Head {
+  kv_u32x4 x[2], o[PAIRS ? 1 : 2];     // 16 elements of a head, and those that they are paired with
+  __device__ __forceinline__ void load(const uint16_t* head, int e0, const Angles<PAIRS>& a) {
+    x[0] = *(const kv_u32x4*)(head + e0);
+    x[1] = *(const kv_u32x4*)(head + e0 + 8);
+    if (!PAIRS) {
+#pragma unroll
+      for (int p = 0; p < 2; p++) o[PAIRS ? 0 : p] = *(const kv_u32x4*)(head + a.other[PAIRS ? 0 : p]);
+    }
+  }
+};
+
+// The lane's 16 elements, normed where there is a weight (of the head's elements) and turned.
+template <int LG, bool PAIRS>
+__device__ __forceinline__ void turned(float (&y)[16], const Head<PAIRS>& h, const Angles<PAIRS>& a, const float* weight, const TurnCtx& c, int e0, bool holds) {
+  float z[PAIRS ? 1 : 16];
+#pragma unroll
+  for (int e = 0; e < 16; e++) {
+    y[e] = bf16_at(h.x[e / 8][e % 8 / 2], e & 1);
+    if (!PAIRS) z[PAIRS ? 0 : e] = bf16_at(h.o[PAIRS ? 0 : e / 8][e % 8 / 2], e & 1);
+  }
+  if (weight) {
+    float sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 16; e++) sum = fmaf(y[e], y[e], sum);
+    sum = group_sum<LG>(holds ? sum : 0.f);
+    const float r = __builtin_amdgcn_rsqf(fmaf(sum, c.inv_d, c.eps));
+#pragma unroll
+    for (int q = 0; q < 4; q++) {
+      const float4 w = *(const float4*)(weight + e0 + 4 * q);
+      y[4 * q] *= r * w.x; y[4 * q + 1] *= r * w.y; y[4 * q + 2] *= r * w.z; y[4 * q + 3] *= r * w.w;
+      if (!PAIRS) {
+        const float4 v = *(const float4*)(weight + a.other[PAIRS ? 0 : q / 2] + 4 * (q % 2));
+        float* zq = z + (PAIRS ? 0 : 4 * q);
+        zq[0] *= r * v.x; zq[PAIRS ? 0 : 1] *= r * v.y; zq[PAIRS ? 0 : 2] *= r * v.z; zq[PAIRS ? 0 : 3] *= r * v.w;
+      }
+    }
+  }
+  if (a.turns) {
+#pragma unroll
+    for (int e = 0; e < 16; e += PAIRS ? 2 : 1) {
+      if (PAIRS) {
+        const float u = y[e], v = y[PAIRS ? e + 1 : e], cs = a.cs[e / 2], sn = a.sn[e / 2];
+        y[e] = fmaf(u, cs, -(v * sn));
+        y[PAIRS ? e + 1 : e] = fmaf(v, cs, u * sn);
+      } else {
+        y[e] = fmaf(y[e], a.cs[PAIRS ? 0 : e], z[PAIRS ? 0 : e] * a.sn[PAIRS ? 0 : e]);
+      }
+    }
+  }
+}
+
+__device__ __forceinline__ void store16(uint16_t* to, const float (&y)[16]) {
+#pragma unroll
+  for (int p = 0; p < 2; p++) {
+    const kv_u32x4 w = {bf16_pair(y[8 * p], y[8 * p + 1]), bf16_pair(y[8 * p + 2], y[8 * p + 3]), bf16_pair(y[8 * p + 4], y[8 * p + 5]), bf16_pair(y[8 * p + 6], y[8 * p + 7])};
+    *(kv_u32x4*)(to + 8 * p) = w;
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ queries and keys
+struct NormRopeCtx {
+  TurnCtx t;
+  int Hq, Hkv, heads;                  // heads: of q, k and v together
+  int64_t q_stride, k_stride, v_stride, q_out_stride, k_out_stride, v_out_stride;
+  const uint16_t* q;
+  const uint16_t* k;
+  const uint16_t* v;
+  const float* q_weight;
+  const float* k_weight;
+  uint16_t* q_out;
+  uint16_t* k_out;
+  uint16_t* v_out;
+};
+
+// U: heads of a wavefront.  In place: a head is read by one wavefront only, whose loads of it all stand before its stores.
+template <int LG, bool PAIRS, int U>
+__global__ void __launch_bounds__(256) k_qk_norm_rope(NormRopeCtx c) {
+  const Place<LG> at(c.t);
+  const Angles<PAIRS> a(c.t, at.at, at.e0);
+  const int h0 = ((int)at.chunk * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6)) * U;
+  Head<PAIRS> x[U];
+#pragma unroll
+  for (int u = 0; u < U; u++) {
+    const int h = min(h0 + u, c.heads - 1);
+    const uint16_t* from = h < c.Hq              ? c.q + (int64_t)at.row * c.q_stride + h * c.t.d
+                           : h < c.Hq + c.Hkv    ? c.k + (int64_t)at.row * c.k_stride + (h - c.Hq) * c.t.d
+                                                 : c.v + (int64_t)at.row * c.v_stride + (h - c.Hq - c.Hkv) * c.t.d;
+    x[u].load(from, at.e0, a);
+  }
+#pragma unroll
+  for (int u = 0; u < U; u++) {
+    const int h = h0 + u;
+    if (h >= c.heads) return;
+    if (h >= c.Hq + c.Hkv) {
+      if (at.live && at.holds) {
+        uint16_t* to = c.v_out + (int64_t)at.row * c.v_out_stride + (h - c.Hq - c.Hkv) * c.t.d + at.e0;
+        *(kv_u32x4*)to = x[u].x[0];
+        *(kv_u32x4*)(to + 8) = x[u].x[1];
+      }
+      continue;
+    }
+    const bool is_q = h < c.Hq;
+    float y[16];
+    turned<LG, PAIRS>(y, x[u], a, is_q ? c.q_weight : c.k_weight, c.t, at.e0, at.holds);
+    uint16_t* to = is_q ? c.q_out + (int64_t)at.row * c.q_out_stride + h * c.t.d : c.k_out + (int64_t)at.row * c.k_out_stride + (h - c.Hq) * c.t.d;
+    if (at.live && at.holds) store16(to + at.e0, y);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ into pages
+struct AppendCtx {
+  TurnCtx t;
+  int Hkv, shift;
+  uint32_t n_slots;
+  int64_t k_stride, v_stride;
+  float k_scale, v_scale, k_rcp, v_rcp;
+  const uint16_t* k;
+  const uint16_t* v;
+  const int32_t* slot;
+  const float* k_weight;
+  uint8_t* k_pages;
+  uint8_t* v_pages;
+};
+
+// 16 values as FP4 (E2M1) codes under the scale of the 32 that this lane and its neighbour hold: the smallest power of two 2^e, -120 <= e <= 125, with |y| <= 7 * 2^e, so
+// that no value is further from its code's than half the distance of the two codes around it (the largest is 6, 7 half a step above it; with 2^(floor(log2 max) - 2),
+// the usual choice, values between 7 and 8 are up to a whole step off).  The bits of 1.75 * 2^k + 0x1fffff are the last that keep their exponent.  An infinite value or NaN among
+// the 32 makes the scale 255, which says NaN for all of them.
+__device__ __forceinline__ kv_u32x2 fp4_codes16(const float (&y)[16], uint32_t* scale) {
+  uint32_t most = 0;
+#pragma unroll
+  for (int e = 0; e < 16; e++) most = max(most, __float_as_uint(y[e]) & 0x7fffffffu);      // (as whole numbers: NaN is above the infinite)
+  most = max(most, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)most, 0xb1, 0xf, 0xf, false));
+  const uint32_t e8 = min(max(((most + 0x1fffffu) >> 23), 9u) - 2u, 252u);
+  *scale = most >= 0x7f800000u ? 255u : e8;
+  const float step = __uint_as_float(e8 << 23);
+  kv_u32x2 w;
+#pragma unroll
+  for (int p = 0; p < 2; p++) {
+    uint32_t v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, y[8 * p], y[8 * p + 1], step, 0);
+    v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, y[8 * p + 2], y[8 * p + 3], step, 1);
+    v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, y[8 * p + 4], y[8 * p + 5], step, 2);
+    w[p] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, y[8 * p + 6], y[8 * p + 7], step, 3);
+  }
+  return w;
+}
+
+// KV: GR_KV_BF16, GR_KV_FP8, GR_KV_FP4, or 3: FP8 under scales that are divided by (see fp8_quotient).
+template <int LG, bool PAIRS, int KV, int U>
+__global__ void __launch_bounds__(256) k_page_append(AppendCtx c) {
+  Place<LG> at(c.t);
+  const uint32_t slot = (uint32_t)c.slot[at.row];
+  at.live = at.live && slot < c.n_slots;
+  const Angles<PAIRS> a(c.t, at.at, at.e0);
+  const int h0 = ((int)at.chunk * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6)) * U, heads = 2 * c.Hkv;
+  Head<PAIRS> x[U];
+#pragma unroll
+  for (int u = 0; u < U; u++) {
+    const int h = min(h0 + u, heads - 1);
+    x[u].load(h < c.Hkv ? c.k + (int64_t)at.row * c.k_stride + h * c.t.d : c.v + (int64_t)at.row * c.v_stride + (h - c.Hkv) * c.t.d, at.e0, a);
+  }
+#pragma unroll
+  for (int u = 0; u < U; u++) {
+    int h = h0 + u;
+    if (h >= heads) return;
+    const bool is_k = h < c.Hkv;
+    h -= is_k ? 0 : c.Hkv;
+    float y[16];
+    if (is_k) {
+      turned<LG, PAIRS>(y, x[u], a, c.k_weight, c.t, at.e0, at.holds);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 16; e++) y[e] = bf16_at(x[u].x[e / 8][e % 8 / 2], e & 1);
+    }
+    uint8_t* pages = is_k ? c.k_pages : c.v_pages;
+    const bool stores = at.live && at.holds;
+    if (KV == GR_KV_FP4) {
+      uint32_t scale;
+      const kv_u32x2 w = fp4_codes16(y, &scale);
+      const uint32_t ps = 1u << c.shift, tok = slot & (ps - 1), d = (uint32_t)c.t.d, e0 = (uint32_t)at.e0;
+      uint8_t* record = pages + ((size_t)(slot >> c.shift) * (unsigned)c.Hkv + (unsigned)h) * gr_fp4_record(ps, d);
+      if (stores) {
+        *(kv_u32x2*)(record + tok * (d / 2) + e0 / 2) = w;
+        if ((e0 & 16) == 0) record[gr_fp4_codes(ps, d) + tok * (d / 32) + e0 / 32] = (uint8_t)scale;
+      }
+    } else {
+      const size_t i = ((size_t)slot * (unsigned)c.Hkv + (unsigned)h) * (unsigned)c.t.d + (unsigned)at.e0;
+      if (KV == GR_KV_BF16) {
+        if (stores) store16((uint16_t*)pages + i, y);
+      } else {
+        const float scale = is_k ? c.k_scale : c.v_scale, rcp = is_k ? c.k_rcp : c.v_rcp;
+        float f[16];
+#pragma unroll
+        for (int e = 0; e < 16; e++) f[e] = fp8_quotient<KV == GR_KV_FP8>(y[e], scale, rcp);
+        const kv_u32x4 w = {fp8_codes4(f[0], f[1], f[2], f[3]), fp8_codes4(f[4], f[5], f[6], f[7]), fp8_codes4(f[8], f[9], f[10], f[11]), fp8_codes4(f[12], f[13], f[14], f[15])};
+        if (stores) *(kv_u32x4*)(pages + i) = w;
+      }
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ host
+bool any_misaligned(std::initializer_list<const void*> of, uintptr_t mask) {
+  for (const void* p : of)
+    if ((uintptr_t)p & mask) return true;
+  return false;
+}
+
+// What both calls ask of a rotation and of a head's size
+gr_status turn_ok(int32_t d, int32_t rot, int32_t pairs, int32_t n_pos, float eps, bool norms, const float* table, const int32_t* pos, int64_t T) {
+  if (d <= 0 || rot < 0 || rot > d || (pairs != 0 && pairs != 1)) return GR_ERR_INVALID_ARG;
+  if (rot > 0 && (n_pos <= 0 || (T > 0 && (!table || !pos)))) return GR_ERR_INVALID_ARG;
+  if (norms && !(eps >= 0.f && eps < INFINITY)) return GR_ERR_INVALID_ARG;
+  if (d % 16 || d > 256 || rot % 16) return GR_ERR_UNSUPPORTED;
+  return GR_OK;
+}
+void fill_turn(TurnCtx* t, int64_t T, int32_t d, int32_t rot, int32_t n_pos, float eps, const float* table, const int32_t* pos) {
+  t->T = (uint32_t)T; t->d = d; t->rot = rot; t->n_pos = n_pos; t->inv_d = 1.0f / (float)d; t->eps = eps; t->table = table; t->pos = pos;
+}
+// The launch: 0 where it has too many threads
+unsigned grid_of(TurnCtx* t, int lg, int heads, int per_wave) {
+  t->chunks = (uint32_t)((heads + 4 * per_wave - 1) / (4 * per_wave));
+  t->inv_chunks = 0xffffffffu / t->chunks;
+  const int64_t rows = 64 / lg, grid = ((int64_t)t->T + rows - 1) / rows * t->chunks;
+  return gr_grid_fits(grid, 256) ? (unsigned)grid : 0;
+}
+int lanes_of_head(int d) { return d <= 64 ? 4 : d <= 128 ? 8 : 16; }
+
+template <class F>
+gr_status with_lanes(int lg, F&& f) {
+  return lg == 4 ? f(std::integral_constant<int, 4>()) : lg == 8 ? f(std::integral_constant<int, 8>()) : f(std::integral_constant<int, 16>());
+}
+template <class F>
+gr_status with_bool(bool b, F&& f) { return b ? f(std::true_type()) : f(std::false_type()); }
+
+}  // namespace
+
+extern "C" gr_status gr_qk_norm_rope(const gr_qk_norm_rope_params* p, void* stream_) {
+  if (!p) return GR_ERR_INVALID_ARG;
+  const bool has_q = p->q != nullptr, has_k = p->k != nullptr, has_v = p->v != nullptr;
+  if (p->T < 0 || p->Hq < 0 || p->Hkv < 0 || (has_q && p->Hq == 0) || ((has_k || has_v) && p->Hkv == 0)) return GR_ERR_INVALID_ARG;
+  if (!has_q && !has_k && p->T > 0) return GR_ERR_INVALID_ARG;
+  if (has_q != (p->q_out != nullptr) || has_k != (p->k_out != nullptr) || has_v != (p->v_out != nullptr)) return GR_ERR_INVALID_ARG;
+  if ((p->q_weight && !has_q) || (p->k_weight && !has_k)) return GR_ERR_INVALID_ARG;
+  if (const gr_status st = turn_ok(p->d, p->rot, p->pairs, p->n_pos, p->eps, p->q_weight || p->k_weight, p->table, p->pos, p->T)) return st;
+  const int64_t nq = (int64_t)p->Hq * p->d, nk = (int64_t)p->Hkv * p->d;
+  if ((has_q && (p->q_stride < nq || p->q_out_stride < nq)) || (has_k && (p->k_stride < nk || p->k_out_stride < nk)) || (has_v && (p->v_stride < nk || p->v_out_stride < nk)))
+    return GR_ERR_INVALID_ARG;
+  if ((p->q_out == p->q && has_q && p->q_out_stride != p->q_stride) || (p->k_out == p->k && has_k && p->k_out_stride != p->k_stride)) return GR_ERR_INVALID_ARG;
+  if (has_v && (p->v_out == p->v || p->v_out == p->k_out || p->v_out == p->q_out)) return GR_ERR_INVALID_ARG;
+  if (has_q && has_k && p->q_out == p->k_out) return GR_ERR_INVALID_ARG;
+  if (any_misaligned({p->q, p->k, p->v, p->q_weight, p->k_weight, p->table, p->q_out, p->k_out, p->v_out}, 15) || any_misaligned({p->pos}, 3)) return GR_ERR_INVALID_ARG;
+  auto odd = [](bool has, int64_t a, int64_t b) { return has && (a % 8 || b % 8); };
+  if (odd(has_q, p->q_stride, p->q_out_stride) || odd(has_k, p->k_stride, p->k_out_stride) || odd(has_v, p->v_stride, p->v_out_stride)) return GR_ERR_UNSUPPORTED;
+  if (p->T >= (int64_t)1 << 31 || nq > 1 << 20 || nk > 1 << 20) return GR_ERR_UNSUPPORTED;
+  if (p->T == 0) return GR_OK;
+  NormRopeCtx c;
+  fill_turn(&c.t, p->T, p->d, p->rot, p->n_pos, p->eps, p->table, p->pos);
+  c.Hq = has_q ? p->Hq : 0; c.Hkv = has_k ? p->Hkv : 0; c.heads = c.Hq + c.Hkv + (has_v ? p->Hkv : 0);
+  c.q_stride = p->q_stride; c.k_stride = p->k_stride; c.v_stride = p->v_stride;
+  c.q_out_stride = p->q_out_stride; c.k_out_stride = p->k_out_stride; c.v_out_stride = p->v_out_stride;
+  c.q = (const uint16_t*)p->q; c.k = (const uint16_t*)p->k; c.v = (const uint16_t*)p->v; c.q_weight = p->q_weight; c.k_weight = p->k_weight;
+  c.q_out = (uint16_t*)p->q_out; c.k_out = (uint16_t*)p->k_out; c.v_out = (uint16_t*)p->v_out;
+  const int lg = lanes_of_head(p->d);
+  const gr_status st = with_lanes(lg, [&](auto lanes) {
+    return with_bool(p->pairs != 0, [&](auto pairs) {
+      const unsigned grid = grid_of(&c.t, lg, c.heads, 1);
+      if (!grid) return (gr_status)GR_ERR_UNSUPPORTED;
+      hipLaunchKernelGGL((k_qk_norm_rope<decltype(lanes)::value, decltype(pairs)::value, 1>), dim3(grid), dim3(256), 0, (hipStream_t)stream_, c);
+      return (gr_status)GR_OK;
+    });
+  });
+  if (st) return st;
+  GR_HIP_TRY(hipGetLastError());
+  return GR_OK;
+}
+
+extern "C" gr_status gr_page_append(const gr_page_append_params* p, void* stream_) {
+  if (!p) return GR_ERR_INVALID_ARG;
+  if (p->T < 0 || p->Hkv <= 0 || p->n_pages <= 0) return GR_ERR_INVALID_ARG;
+  if (p->kv_type != GR_KV_BF16 && p->kv_type != GR_KV_FP8 && p->kv_type != GR_KV_FP4) return GR_ERR_INVALID_ARG;
+  if (p->kv_type == GR_KV_FP8 && (!gr_scale_ok(p->k_scale) || !gr_scale_ok(p->v_scale))) return GR_ERR_INVALID_ARG;
+  if (!p->k_pages || !p->v_pages || p->k_pages == p->v_pages) return GR_ERR_INVALID_ARG;
+  if (p->T > 0 && (!p->k || !p->v || !p->slot)) return GR_ERR_INVALID_ARG;
+  if (const gr_status st = turn_ok(p->d, p->rot, p->pairs, p->n_pos, p->eps, p->k_weight != nullptr, p->table, p->pos, p->T)) return st;
+  const int64_t n = (int64_t)p->Hkv * p->d;
+  if (p->k_stride < n || p->v_stride < n) return GR_ERR_INVALID_ARG;
+  if (any_misaligned({p->k, p->v, p->k_pages, p->v_pages, p->k_weight, p->table}, 15) || any_misaligned({p->slot, p->pos}, 3)) return GR_ERR_INVALID_ARG;
+  if (!gr_page_size_ok(p->page_size) || p->k_stride % 8 || p->v_stride % 8 || n > 1 << 20) return GR_ERR_UNSUPPORTED;
+  if (p->kv_type == GR_KV_FP4 && p->d % 32) return GR_ERR_UNSUPPORTED;
+  if ((int64_t)p->n_pages * p->page_size >= ((int64_t)1 << 31) || p->T >= ((int64_t)1 << 31)) return GR_ERR_UNSUPPORTED;
+  if (p->T == 0) return GR_OK;
+  AppendCtx c;
+  fill_turn(&c.t, p->T, p->d, p->rot, p->n_pos, p->eps, p->table, p->pos);
+  c.Hkv = p->Hkv; c.shift = __builtin_ctz((unsigned)p->page_size); c.n_slots = (uint32_t)(p->n_pages * p->page_size);
+  c.k_stride = p->k_stride; c.v_stride = p->v_stride; c.k_scale = p->k_scale; c.v_scale = p->v_scale; c.k_rcp = 1.0f / p->k_scale; c.v_rcp = 1.0f / p->v_scale;
+  c.k = (const uint16_t*)p->k; c.v = (const uint16_t*)p->v; c.slot = p->slot; c.k_weight = p->k_weight; c.k_pages = (uint8_t*)p->k_pages; c.v_pages = (uint8_t*)p->v_pages;
+  auto ordinary = [](float s) { return s >= 0x1p-60f && s <= 0x1p60f; };
+  const int lg = lanes_of_head(p->d);
+  const gr_status st = with_lanes(lg, [&](auto lanes) {
+    return with_bool(p->pairs != 0, [&](auto pairs) {
+      auto go = [&](auto type) {
+        const unsigned grid = grid_of(&c.t, lg, 2 * p->Hkv, 1);
+        if (!grid) return (gr_status)GR_ERR_UNSUPPORTED;
+        hipLaunchKernelGGL((k_page_append<decltype(lanes)::value, decltype(pairs)::value, decltype(type)::value, 1>), dim3(grid), dim3(256), 0, (hipStream_t)stream_, c);
+        return (gr_status)GR_OK;
+      };
+      if (p->kv_type == GR_KV_BF16) return go(std::integral_constant<int, GR_KV_BF16>());
+      if (p->kv_type == GR_KV_FP4) return go(std::integral_constant<int, GR_KV_FP4>());
+      if (ordinary(p->k_scale) && ordinary(p->v_scale)) return go(std::integral_constant<int, GR_KV_FP8>());
+      return go(std::integral_constant<int, 3>());
+    });
+  });
+  if (st) return st;
+  GR_HIP_TRY(hipGetLastError());
+  return GR_OK;
+}
