@@ -436,7 +436,7 @@ gr_status gr_page_read(const gr_page_read_params* p, void* stream);
  * prefix is read and multiplied once for the rows of all requests; with more, each request's rows meet it by themselves.
  * What a table holds beyond a request's pages is of no effect; a page number outside [0, n_pages) is read as page 0, and a length outside [0, max_L] as the
  * nearer end.  Slots of a page behind a request's last token may hold anything.
- * GR_KV_FP8: pools of E4M3 codes, scales applied as in gr_beam_attn_fp8kv.
+ * GR_KV_FP8: pools of E4M3 codes, scales applied as in gr_beam_attn_fp8kv.  GR_KV_FP4: codes are widened with their blocks' scales to bf16, exactly (scales 2^-120 to 2^125).
  * Supported: d in {64, 128}; Hq % Hkv == 0; 0 <= u <= ND; prefix_L a multiple of page_size; n_pages * page_size below 2^31, and that times
  * Hkv * d below 2^41; prefix_L + max_L below 2^30; Hkv * d <= 65536; W * Hq/Hkv < 2^22.  bf16 tensors and pools 16-byte aligned; finite values in the slots that are read; |v| * 2^8 * (number of keys) below 2^128.
  * Workspace (device, 256-byte aligned, contents unspecified before and after): partial results of segments, where a row's keys are split.
@@ -451,7 +451,7 @@ typedef struct {
   float   sm_scale;               /* positive and finite                                               */
   float   k_scale, v_scale;       /* GR_KV_FP8: positive and finite                                    */
   const void*    q;               /* bf16 [B, W, Hq, d]                                                */
-  const void*    k_pages;         /* bf16 or uint8 [n_pages, page_size, Hkv, d]                        */
+  const void*    k_pages;         /* bf16 or uint8 [n_pages, page_size, Hkv, d], or GR_KV_FP4's pools  */
   const void*    v_pages;
   const int32_t* prefix_pages;    /* int32 [prefix_L / page_size]; may be NULL when prefix_L == 0      */
   const int32_t* block_table;     /* int32 [B, max_pages]; may be NULL when max_L == 0                 */
@@ -518,7 +518,7 @@ gr_status gr_logits_adjust(const gr_logits_adjust_params* p, void* stream);
  *   K/V tiles in the longest prompt) prompt segments instead of the built-in launch rule; (0, 0) restores the rule.
  *   For sweeps that refit the rule; not thread-safe against concurrent gr_beam_attn calls.
  * gr_diag_attn_paged_plan: host only.  How gr_beam_attn_paged launches a call of these shapes (of what gr_beam_attn_paged_workspace_bytes looks at), as five
- *   numbers in host memory: query rows of a workgroup that meets requests' own lists (32, 128 or 256), segments of the prefix where the rows of all requests
+ *   numbers in host memory: query rows of a workgroup that meets requests' own lists (32, 128 or 256; GR_KV_FP4 also 16), segments of the prefix where the rows of all requests
  *   meet it together (0: every row walks its whole list), segments of a list, sets of wavefronts of a workgroup (1 or 2), and 1 where workgroups look for
  *   the longest request first.  For tests that have to reach every kernel.
  * gr_diag_issue_loop: the issue test behind the attention kernel's roofline discussion.  `workgroups` x 8 wavefronts

@@ -432,23 +432,25 @@ def gr_page_read(k_pages, v_pages, slot, k, v, k_scale=1.0, v_scale=1.0, stream=
     return k, v
 
 
-def attn_paged_workspace_bytes(B, W, Hq, Hkv, d, max_L, prefix_L=0, fp8=False, page_size=16) -> int:
+def attn_paged_workspace_bytes(B, W, Hq, Hkv, d, max_L, prefix_L=0, fp8=False, page_size=16, fp4=False) -> int:
     """Workspace bytes of gr_beam_attn_paged (the same for pages of any size) with this max_L and prefix_L; shorter ones may need more.  A call's max_L may be larger than its
     lengths."""
-    p = _paged_shapes(B, W, Hq, Hkv, d, max_L, prefix_L, fp8, page_size)
+    p = _paged_shapes(B, W, Hq, Hkv, d, max_L, prefix_L, fp8, page_size, fp4)
     return int(load_library().gr_beam_attn_paged_workspace_bytes(ctypes.byref(p)))
 
 
-def _paged_shapes(B, W, Hq, Hkv, d, max_L, prefix_L, fp8, page_size):
+def _paged_shapes(B, W, Hq, Hkv, d, max_L, prefix_L, fp8, page_size, fp4=False):
+    if fp8 and fp4:
+        raise ValueError("fp8 and fp4: expected one of them at most")
     p = _AttnPagedParams()
-    p.B, p.W, p.Hq, p.Hkv, p.d, p.max_L, p.prefix_L, p.kv_type, p.page_size = B, W, Hq, Hkv, d, int(max_L), int(prefix_L), int(bool(fp8)), int(page_size)
+    p.B, p.W, p.Hq, p.Hkv, p.d, p.max_L, p.prefix_L, p.kv_type, p.page_size = B, W, Hq, Hkv, d, int(max_L), int(prefix_L), 2 if fp4 else int(bool(fp8)), int(page_size)
     return p
 
 
 def gr_beam_attn_paged(q, k_pages, v_pages, block_table, seq_lens, k_unshared, v_unshared, u, sm_scale, max_L, prefix_pages=None, prefix_L=0, k_scale=1.0,
                        v_scale=1.0, slot=None, out=None, lse_out=None, workspace=None, stream=None):
-    """Beam attention over a prompt cache in pages.  q bf16 [B,W,Hq,d]; k/v_pages [n_pages,page_size,Hkv,d], bf16 or uint8 (E4M3 codes, value = code * scale);
-    block_table int32 [B,max_pages]; seq_lens int32 [B]; k/v_unshared bf16 [B,W,ND,Hkv,d] (None: no own tokens, u = 0); `slot` as for gr_beam_attn_slots.
+    """Beam attention over a prompt cache in pages.  q bf16 [B,W,Hq,d]; k/v_pages [n_pages,page_size,Hkv,d], bf16 or uint8 (E4M3 codes, value = code * scale),
+    or uint8 [n_pages,Hkv,kv_fp4_page_bytes(page_size,d)] (FP4); block_table int32 [B,max_pages]; seq_lens int32 [B]; k/v_unshared bf16 [B,W,ND,Hkv,d] (None: no own tokens, u = 0); `slot` as for gr_beam_attn_slots.
     prefix_pages int32 [prefix_L/page_size]: pages of the tokens in front that all requests share.  max_L (the largest of seq_lens, or more) and prefix_L are host
     integers.  Returns (out bf16 [B,W,Hq,d], lse fp32 [B,W,Hq] or None).  Enqueues on `stream` (default: current)."""
     native = _native or _marshal()
@@ -486,10 +488,10 @@ def gr_diag_attn_plan(rows_per_workgroup=0, l_segments=0):
         raise GrError(rc, "gr_diag_attn_plan")
 
 
-def gr_diag_attn_paged_plan(B, W, Hq, Hkv, d, max_L, prefix_L=0, fp8=False, page_size=16):
+def gr_diag_attn_paged_plan(B, W, Hq, Hkv, d, max_L, prefix_L=0, fp8=False, page_size=16, fp4=False):
     """How gr_beam_attn_paged launches such a call: (rows of a workgroup, segments of a prefix met by all requests' rows together or 0, segments of a list, sets of
     wavefronts, longest request first)."""
-    p = _paged_shapes(B, W, Hq, Hkv, d, max_L, prefix_L, fp8, page_size)
+    p = _paged_shapes(B, W, Hq, Hkv, d, max_L, prefix_L, fp8, page_size, fp4)
     plan = (ctypes.c_int32 * 5)()
     rc = load_library().gr_diag_attn_paged_plan(ctypes.byref(p), plan)
     if rc != 0:

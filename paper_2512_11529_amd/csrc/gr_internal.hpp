@@ -28,6 +28,9 @@ static inline gr_status gr_allow_lds(size_t bytes) {
 // The size of a launch in threads is a 32-bit number.
 static inline bool gr_grid_fits(int64_t workgroups, int64_t threads) { return workgroups * threads < ((int64_t)1 << 32); }
 
+// gr_beam_attn_paged over pages in FP4 (gr_paged4.hip), for arguments that it has looked at.
+__attribute__((visibility("hidden"))) gr_status gr_paged_fp4(const gr_attn_paged_params* p, void* workspace, size_t workspace_bytes, hipStream_t stream);
+
 static inline size_t gr_align256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // ------------------------------------------------------------------ mask blob layout
