@@ -4,9 +4,9 @@
 //     y_a' = y_a cos - y_b sin,   y_b' = y_b cos + y_a sin,
 // with (a, b) = (i, i + rot / 2) or (2 i, 2 i + 1) for i < rot / 2.  All of it is in fp32; the only rounding to fewer bits is the store's.
 //
-// Bound: memory, 4 bytes an element in and out (bf16).  A lane holds 16 consecutive elements of a head, 4, 8 or 16 lanes the head, and a wavefront the same head of
-// 16, 8 or 4 consecutive rows: what it writes into an FP4 page is then one run of codes and one of scales, whole 32-byte sectors, and a lane's cosines and sines serve
-// all of its heads.  The wavefronts of a workgroup take different heads of the same rows.  The other halves of pairs (i, i + rot / 2) are loaded a second time, from L1.
+// Bound: memory, 4 bytes an element in and out (bf16).  A lane holds 16 elements of a head in two runs of eight, so that both of every pair are its own: elements 8 j .. and
+// rot / 2 + 8 j .., or 16 j .. .  4, 8 or 16 lanes hold the head, and a wavefront the same head of 16, 8 or 4 consecutive rows: what it writes into an FP4 page is then one
+// run of codes and one of scales, and a lane's cosines and sines serve all of its heads.  The wavefronts of a workgroup take different heads of the same rows.
 #include <initializer_list>
 #include <type_traits>
 #include "gr_pages.hpp"
@@ -41,126 +41,105 @@ struct TurnCtx {
 };
 
 // A wavefront's rows and a lane's part of them.
-template <int LG>
+template <int LG, bool PAIRS>
 struct Place {
   uint32_t row, chunk;                 // (rows past the last one as that one)
-  int at, e0;                          // position; first of the lane's elements
-  bool live, holds;                    // the row is written; the head has these elements
+  int at, e[2];                        // position; first of the lane's elements, of each eight
+  bool live, holds, turns;             // the row is written; the head has these elements; they are rotated
   __device__ __forceinline__ Place(const TurnCtx& c) {
     const uint32_t group = div_by(blockIdx.x, c.chunks, c.inv_chunks);
-    const int lane = (int)threadIdx.x & 63;
+    const int lane = (int)threadIdx.x & 63, j = lane % LG;
     chunk = blockIdx.x - group * c.chunks;
     row = group * (64 / LG) + (uint32_t)(lane / LG);
     live = row < c.T;
     row = min(row, c.T - 1);
-    e0 = (lane % LG) * 16;
-    holds = e0 < c.d;
+    holds = 16 * j < c.d;
+    turns = 16 * j < c.rot;
+    const bool split = !PAIRS && turns;
+    e[0] = holds ? (split ? 8 : 16) * j : 0;                                    // (lanes past the head load what the first does)
+    e[1] = split ? (c.rot >> 1) + e[0] : e[0] + 8;
     at = 0;
     if (c.rot > 0) {
       at = c.pos[row];
       if ((unsigned)at >= (unsigned)c.n_pos) { live = false; at = 0; }
     }
-    if (!holds) e0 = 0;                // (loads what the first lane does)
   }
 };
 
-// Cosines and sines of a lane's 16 elements; of pairs (2 i, 2 i + 1) one for two.
-template <bool PAIRS>
+__device__ __forceinline__ void load8(const float* p, float* to) {
+  const float4 a = *(const float4*)p, b = *(const float4*)(p + 4);
+  to[0] = a.x; to[1] = a.y; to[2] = a.z; to[3] = a.w; to[4] = b.x; to[5] = b.y; to[6] = b.z; to[7] = b.w;
+}
+
+// Cosines and sines of a lane's eight pairs.
 struct Angles {
-  float cs[PAIRS ? 8 : 16], sn[PAIRS ? 8 : 16];
-  int other[PAIRS ? 1 : 2];            // first of the elements that its two eights are paired with
-  bool turns;
-  __device__ __forceinline__ Angles(const TurnCtx& c, int at, int e0) {
-    turns = e0 < c.rot;
-    const int half = c.rot >> 1;
-    const float* t = c.table + (size_t)(unsigned)at * (unsigned)c.rot;
-    auto load8 = [](const float* p, float* to) {
-      const float4 a = *(const float4*)p, b = *(const float4*)(p + 4);
-      to[0] = a.x; to[1] = a.y; to[2] = a.z; to[3] = a.w; to[4] = b.x; to[5] = b.y; to[6] = b.z; to[7] = b.w;
-    };
-    if (PAIRS) {
-      if (turns) {
-        load8(t + (e0 >> 1), cs);
-        load8(t + half + (e0 >> 1), sn);
-      }
-      return;
-    }
-#pragma unroll
-    for (int p = 0; p < 2; p++) {      // (rot is a multiple of 16: eight elements are all in the same half)
-      const int e = e0 + 8 * p;
-      const bool low = e < half;
-      const int i = low ? e : e - half;
-      other[PAIRS ? 0 : p] = turns ? (low ? e + half : i) : e;
-      if (turns) {
-        load8(t + i, cs + (PAIRS ? 0 : 8 * p));
-        load8(t + half + i, sn + (PAIRS ? 0 : 8 * p));
-        if (low) {
-#pragma unroll
-          for (int k = 0; k < 8; k++) sn[PAIRS ? k : 8 * p + k] = -sn[PAIRS ? k : 8 * p + k];
-        }
-      }
-    }
+  float cs[8], sn[8];
+  template <class P>
+  __device__ __forceinline__ Angles(const TurnCtx& c, const P& p, bool pairs) {
+    if (!p.turns) return;
+    const float* t = c.table + (size_t)(unsigned)p.at * (unsigned)c.rot + (pairs ? p.e[0] >> 1 : p.e[0]);
+    load8(t, cs);
+    load8(t + (c.rot >> 1), sn);
   }
 };
 
-template <bool PAIRS>
 struct Head {
-  kv_u32x4 x[2], o[PAIRS ? 1 : 2];     // 16 elements of a head, and those that they are paired with
-  __device__ __forceinline__ void load(const uint16_t* head, int e0, const Angles<PAIRS>& a) {
-    x[0] = *(const kv_u32x4*)(head + e0);
-    x[1] = *(const kv_u32x4*)(head + e0 + 8);
-    if (!PAIRS) {
+  kv_u32x4 x[2];
+  template <class P>
+  __device__ __forceinline__ void load(const uint16_t* head, const P& p) {
+    x[0] = *(const kv_u32x4*)(head + p.e[0]);
+    x[1] = *(const kv_u32x4*)(head + p.e[1]);
+  }
+  __device__ __forceinline__ void numbers(float (&y)[16]) const {
 #pragma unroll
-      for (int p = 0; p < 2; p++) o[PAIRS ? 0 : p] = *(const kv_u32x4*)(head + a.other[PAIRS ? 0 : p]);
-    }
+    for (int e = 0; e < 16; e++) y[e] = bf16_at(x[e / 8][e % 8 / 2], e & 1);
+  }
+};
+
+// A norm's weights for the lane's elements; a wavefront's next head mostly has the same.
+struct Weights {
+  const float* from = nullptr;
+  float w[16];
+  template <class P>
+  __device__ __forceinline__ void of(const float* weight, const P& p) {
+    if (weight == from || !weight) return;
+    from = weight;
+    load8(weight + p.e[0], w);
+    load8(weight + p.e[1], w + 8);
   }
 };
 
 // The lane's 16 elements, normed where there is a weight (of the head's elements) and turned.
 template <int LG, bool PAIRS>
-__device__ __forceinline__ void turned(float (&y)[16], const Head<PAIRS>& h, const Angles<PAIRS>& a, const float* weight, const TurnCtx& c, int e0, bool holds) {
-  float z[PAIRS ? 1 : 16];
-#pragma unroll
-  for (int e = 0; e < 16; e++) {
-    y[e] = bf16_at(h.x[e / 8][e % 8 / 2], e & 1);
-    if (!PAIRS) z[PAIRS ? 0 : e] = bf16_at(h.o[PAIRS ? 0 : e / 8][e % 8 / 2], e & 1);
-  }
+__device__ __forceinline__ void turned(float (&y)[16], const Head& h, const Angles& a, const float* weight, Weights& ws, const TurnCtx& c, const Place<LG, PAIRS>& p) {
+  h.numbers(y);
+  ws.of(weight, p);
   if (weight) {
     float sum = 0.f;
 #pragma unroll
     for (int e = 0; e < 16; e++) sum = fmaf(y[e], y[e], sum);
-    sum = group_sum<LG>(holds ? sum : 0.f);
+    sum = group_sum<LG>(p.holds ? sum : 0.f);
     const float r = __builtin_amdgcn_rsqf(fmaf(sum, c.inv_d, c.eps));
 #pragma unroll
-    for (int q = 0; q < 4; q++) {
-      const float4 w = *(const float4*)(weight + e0 + 4 * q);
-      y[4 * q] *= r * w.x; y[4 * q + 1] *= r * w.y; y[4 * q + 2] *= r * w.z; y[4 * q + 3] *= r * w.w;
-      if (!PAIRS) {
-        const float4 v = *(const float4*)(weight + a.other[PAIRS ? 0 : q / 2] + 4 * (q % 2));
-        float* zq = z + (PAIRS ? 0 : 4 * q);
-        zq[0] *= r * v.x; zq[PAIRS ? 0 : 1] *= r * v.y; zq[PAIRS ? 0 : 2] *= r * v.z; zq[PAIRS ? 0 : 3] *= r * v.w;
-      }
-    }
+    for (int e = 0; e < 16; e++) y[e] *= r * ws.w[e];
   }
-  if (a.turns) {
+  if (p.turns) {
 #pragma unroll
-    for (int e = 0; e < 16; e += PAIRS ? 2 : 1) {
-      if (PAIRS) {
-        const float u = y[e], v = y[PAIRS ? e + 1 : e], cs = a.cs[e / 2], sn = a.sn[e / 2];
-        y[e] = fmaf(u, cs, -(v * sn));
-        y[PAIRS ? e + 1 : e] = fmaf(v, cs, u * sn);
-      } else {
-        y[e] = fmaf(y[e], a.cs[PAIRS ? 0 : e], z[PAIRS ? 0 : e] * a.sn[PAIRS ? 0 : e]);
-      }
+    for (int k = 0; k < 8; k++) {
+      const int i = PAIRS ? 2 * k : k, j = PAIRS ? 2 * k + 1 : k + 8;
+      const float u = y[i], v = y[j];
+      y[i] = fmaf(u, a.cs[k], -(v * a.sn[k]));
+      y[j] = fmaf(v, a.cs[k], u * a.sn[k]);
     }
   }
 }
 
-__device__ __forceinline__ void store16(uint16_t* to, const float (&y)[16]) {
+template <class P>
+__device__ __forceinline__ void store16(uint16_t* head, const P& p, const float (&y)[16]) {
 #pragma unroll
-  for (int p = 0; p < 2; p++) {
-    const kv_u32x4 w = {bf16_pair(y[8 * p], y[8 * p + 1]), bf16_pair(y[8 * p + 2], y[8 * p + 3]), bf16_pair(y[8 * p + 4], y[8 * p + 5]), bf16_pair(y[8 * p + 6], y[8 * p + 7])};
-    *(kv_u32x4*)(to + 8 * p) = w;
+  for (int r = 0; r < 2; r++) {
+    const kv_u32x4 w = {bf16_pair(y[8 * r], y[8 * r + 1]), bf16_pair(y[8 * r + 2], y[8 * r + 3]), bf16_pair(y[8 * r + 4], y[8 * r + 5]), bf16_pair(y[8 * r + 6], y[8 * r + 7])};
+    *(kv_u32x4*)(head + p.e[r]) = w;
   }
 }
 
@@ -179,38 +158,39 @@ struct NormRopeCtx {
   uint16_t* v_out;
 };
 
-// U: heads of a wavefront.  In place: a head is read by one wavefront only, whose loads of it all stand before its stores.
+// U: heads of a wavefront.  In place: a lane reads and writes the same elements.
 template <int LG, bool PAIRS, int U>
 __global__ void __launch_bounds__(256) k_qk_norm_rope(NormRopeCtx c) {
-  const Place<LG> at(c.t);
-  const Angles<PAIRS> a(c.t, at.at, at.e0);
+  const Place<LG, PAIRS> at(c.t);
   const int h0 = ((int)at.chunk * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6)) * U;
-  Head<PAIRS> x[U];
+  Head x[U];
 #pragma unroll
   for (int u = 0; u < U; u++) {
     const int h = min(h0 + u, c.heads - 1);
-    const uint16_t* from = h < c.Hq              ? c.q + (int64_t)at.row * c.q_stride + h * c.t.d
-                           : h < c.Hq + c.Hkv    ? c.k + (int64_t)at.row * c.k_stride + (h - c.Hq) * c.t.d
-                                                 : c.v + (int64_t)at.row * c.v_stride + (h - c.Hq - c.Hkv) * c.t.d;
-    x[u].load(from, at.e0, a);
+    x[u].load(h < c.Hq              ? c.q + (int64_t)at.row * c.q_stride + h * c.t.d
+              : h < c.Hq + c.Hkv    ? c.k + (int64_t)at.row * c.k_stride + (h - c.Hq) * c.t.d
+                                    : c.v + (int64_t)at.row * c.v_stride + (h - c.Hq - c.Hkv) * c.t.d, at);
   }
+  const Angles a(c.t, at, PAIRS);
+  Weights ws;
+  const bool stores = at.live && at.holds;
 #pragma unroll
   for (int u = 0; u < U; u++) {
     const int h = h0 + u;
     if (h >= c.heads) return;
     if (h >= c.Hq + c.Hkv) {
-      if (at.live && at.holds) {
-        uint16_t* to = c.v_out + (int64_t)at.row * c.v_out_stride + (h - c.Hq - c.Hkv) * c.t.d + at.e0;
-        *(kv_u32x4*)to = x[u].x[0];
-        *(kv_u32x4*)(to + 8) = x[u].x[1];
+      uint16_t* to = c.v_out + (int64_t)at.row * c.v_out_stride + (h - c.Hq - c.Hkv) * c.t.d;
+      if (stores) {
+        *(kv_u32x4*)(to + at.e[0]) = x[u].x[0];
+        *(kv_u32x4*)(to + at.e[1]) = x[u].x[1];
       }
       continue;
     }
     const bool is_q = h < c.Hq;
     float y[16];
-    turned<LG, PAIRS>(y, x[u], a, is_q ? c.q_weight : c.k_weight, c.t, at.e0, at.holds);
+    turned<LG, PAIRS>(y, x[u], a, is_q ? c.q_weight : c.k_weight, ws, c.t, at);
     uint16_t* to = is_q ? c.q_out + (int64_t)at.row * c.q_out_stride + h * c.t.d : c.k_out + (int64_t)at.row * c.k_out_stride + (h - c.Hq) * c.t.d;
-    if (at.live && at.holds) store16(to + at.e0, y);
+    if (stores) store16(to, at, y);
   }
 }
 
@@ -229,43 +209,36 @@ struct AppendCtx {
   uint8_t* v_pages;
 };
 
-// 16 values as FP4 (E2M1) codes under the scale of the 32 that this lane and its neighbour hold: the smallest power of two 2^e, -120 <= e <= 125, with |y| <= 7 * 2^e, so
-// that no value is further from its code's than half the distance of the two codes around it (the largest is 6, 7 half a step above it; with 2^(floor(log2 max) - 2),
-// the usual choice, values between 7 and 8 are up to a whole step off).  The bits of 1.75 * 2^k + 0x1fffff are the last that keep their exponent.  An infinite value or NaN among
-// the 32 makes the scale 255, which says NaN for all of them.
-__device__ __forceinline__ kv_u32x2 fp4_codes16(const float (&y)[16], uint32_t* scale) {
-  uint32_t most = 0;
-#pragma unroll
-  for (int e = 0; e < 16; e++) most = max(most, __float_as_uint(y[e]) & 0x7fffffffu);      // (as whole numbers: NaN is above the infinite)
-  most = max(most, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)most, 0xb1, 0xf, 0xf, false));
-  const uint32_t e8 = min(max(((most + 0x1fffffu) >> 23), 9u) - 2u, 252u);
-  *scale = most >= 0x7f800000u ? 255u : e8;
-  const float step = __uint_as_float(e8 << 23);
-  kv_u32x2 w;
-#pragma unroll
-  for (int p = 0; p < 2; p++) {
-    uint32_t v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, y[8 * p], y[8 * p + 1], step, 0);
-    v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, y[8 * p + 2], y[8 * p + 3], step, 1);
-    v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, y[8 * p + 4], y[8 * p + 5], step, 2);
-    w[p] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, y[8 * p + 6], y[8 * p + 7], step, 3);
-  }
-  return w;
+// FP4: the scale of 32 values is the smallest power of two 2^e, -120 <= e <= 125, with |y| <= 7 * 2^e, so that no value is further from its code's than half the distance of the two
+// codes around it (the largest is 6, 7 half a step above it; with 2^(floor(log2 max) - 2), the usual choice, values between 7 and 8 are up to a whole step off).  `most`: the bits of the
+// largest, of which 1.75 * 2^k + 0x1fffff are the last that keep their exponent.
+__device__ __forceinline__ uint32_t fp4_power(uint32_t most) { return min(max((most + 0x1fffffu) >> 23, 9u) - 2u, 252u); }
+// Eight values as codes under the scale 2^(power - 127), to nearest, ties to even
+__device__ __forceinline__ uint32_t fp4_codes8(const float* y, uint32_t power) {
+  const float step = __uint_as_float(power << 23);
+  uint32_t v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, y[0], y[1], step, 0);
+  v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, y[2], y[3], step, 1);
+  v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, y[4], y[5], step, 2);
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, y[6], y[7], step, 3);
 }
 
 // KV: GR_KV_BF16, GR_KV_FP8, GR_KV_FP4, or 3: FP8 under scales that are divided by (see fp8_quotient).
 template <int LG, bool PAIRS, int KV, int U>
 __global__ void __launch_bounds__(256) k_page_append(AppendCtx c) {
-  Place<LG> at(c.t);
+  const Place<LG, PAIRS> at(c.t);
   const uint32_t slot = (uint32_t)c.slot[at.row];
-  at.live = at.live && slot < c.n_slots;
-  const Angles<PAIRS> a(c.t, at.at, at.e0);
-  const int h0 = ((int)at.chunk * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6)) * U, heads = 2 * c.Hkv;
-  Head<PAIRS> x[U];
+  const bool stores = at.live && at.holds && slot < c.n_slots;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), h0 = ((int)at.chunk * 4 + wave) * U, heads = 2 * c.Hkv;
+  Head x[U];
 #pragma unroll
   for (int u = 0; u < U; u++) {
     const int h = min(h0 + u, heads - 1);
-    x[u].load(h < c.Hkv ? c.k + (int64_t)at.row * c.k_stride + h * c.t.d : c.v + (int64_t)at.row * c.v_stride + (h - c.Hkv) * c.t.d, at.e0, a);
+    x[u].load(h < c.Hkv ? c.k + (int64_t)at.row * c.k_stride + h * c.t.d : c.v + (int64_t)at.row * c.v_stride + (h - c.Hkv) * c.t.d, at);
   }
+  const Angles a(c.t, at, PAIRS);
+  Weights ws;
+  // largest of each eight of the wavefront's heads: a block's are four neighbours there, wherever its lanes are
+  __shared__ __attribute__((aligned(16))) uint32_t s_most[KV == GR_KV_FP4 ? 4 * 128 : 4];
 #pragma unroll
   for (int u = 0; u < U; u++) {
     int h = h0 + u;
@@ -273,34 +246,49 @@ __global__ void __launch_bounds__(256) k_page_append(AppendCtx c) {
     const bool is_k = h < c.Hkv;
     h -= is_k ? 0 : c.Hkv;
     float y[16];
-    if (is_k) {
-      turned<LG, PAIRS>(y, x[u], a, c.k_weight, c.t, at.e0, at.holds);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 16; e++) y[e] = bf16_at(x[u].x[e / 8][e % 8 / 2], e & 1);
-    }
+    if (is_k) turned<LG, PAIRS>(y, x[u], a, c.k_weight, ws, c.t, at);
+    else x[u].numbers(y);
     uint8_t* pages = is_k ? c.k_pages : c.v_pages;
-    const bool stores = at.live && at.holds;
     if (KV == GR_KV_FP4) {
-      uint32_t scale;
-      const kv_u32x2 w = fp4_codes16(y, &scale);
-      const uint32_t ps = 1u << c.shift, tok = slot & (ps - 1), d = (uint32_t)c.t.d, e0 = (uint32_t)at.e0;
-      uint8_t* record = pages + ((size_t)(slot >> c.shift) * (unsigned)c.Hkv + (unsigned)h) * gr_fp4_record(ps, d);
-      if (stores) {
-        *(kv_u32x2*)(record + tok * (d / 2) + e0 / 2) = w;
-        if ((e0 & 16) == 0) record[gr_fp4_codes(ps, d) + tok * (d / 32) + e0 / 32] = (uint8_t)scale;
+      const uint32_t ps = 1u << c.shift, tok = slot & (ps - 1), d = (uint32_t)c.t.d;
+      uint32_t* most = s_most + wave * 128 + ((int)threadIdx.x & 63) / LG * (2 * LG);
+      if (at.holds) {
+#pragma unroll
+        for (int r = 0; r < 2; r++) {
+          uint32_t m = 0;
+#pragma unroll
+          for (int e = 0; e < 8; e++) m = max(m, __float_as_uint(y[8 * r + e]) & 0x7fffffffu);       // (as whole numbers: NaN is above the infinite)
+          most[at.e[r] >> 3] = m;
+        }
       }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");             // (the wavefront's own places, and LDS serves it in order)
+      uint8_t* record = pages + ((size_t)(slot >> c.shift) * (unsigned)c.Hkv + (unsigned)h) * gr_fp4_record(ps, d);
+#pragma unroll
+      for (int r = 0; r < 2; r++) {
+        const uint32_t e = (uint32_t)at.e[r];
+        const uint4 m4 = *(const uint4*)(most + (e >> 5) * 4);
+        const uint32_t m = max(max(m4.x, m4.y), max(m4.z, m4.w)), power = fp4_power(m);
+        if (stores) {
+          *(uint32_t*)(record + tok * (d / 2) + e / 2) = fp4_codes8(y + 8 * r, power);
+          // (an infinite value or NaN makes the scale one that says NaN for all 32)
+          if ((e & 31) == 0) record[gr_fp4_codes(ps, d) + tok * (d / 32) + e / 32] = (uint8_t)(m >= 0x7f800000u ? 255u : power);
+        }
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     } else {
-      const size_t i = ((size_t)slot * (unsigned)c.Hkv + (unsigned)h) * (unsigned)c.t.d + (unsigned)at.e0;
+      const size_t i = ((size_t)slot * (unsigned)c.Hkv + (unsigned)h) * (unsigned)c.t.d;
       if (KV == GR_KV_BF16) {
-        if (stores) store16((uint16_t*)pages + i, y);
+        if (stores) store16((uint16_t*)pages + i, at, y);
       } else {
         const float scale = is_k ? c.k_scale : c.v_scale, rcp = is_k ? c.k_rcp : c.v_rcp;
-        float f[16];
 #pragma unroll
-        for (int e = 0; e < 16; e++) f[e] = fp8_quotient<KV == GR_KV_FP8>(y[e], scale, rcp);
-        const kv_u32x4 w = {fp8_codes4(f[0], f[1], f[2], f[3]), fp8_codes4(f[4], f[5], f[6], f[7]), fp8_codes4(f[8], f[9], f[10], f[11]), fp8_codes4(f[12], f[13], f[14], f[15])};
-        if (stores) *(kv_u32x4*)(pages + i) = w;
+        for (int r = 0; r < 2; r++) {
+          float f[8];
+#pragma unroll
+          for (int e = 0; e < 8; e++) f[e] = fp8_quotient<KV == GR_KV_FP8>(y[8 * r + e], scale, rcp);
+          const kv_u32x2 w = {fp8_codes4(f[0], f[1], f[2], f[3]), fp8_codes4(f[4], f[5], f[6], f[7])};
+          if (stores) *(kv_u32x2*)(pages + i + at.e[r]) = w;
+        }
       }
     }
   }
@@ -337,6 +325,13 @@ template <class F>
 gr_status with_lanes(int lg, F&& f) {
   return lg == 4 ? f(std::integral_constant<int, 4>()) : lg == 8 ? f(std::integral_constant<int, 8>()) : f(std::integral_constant<int, 16>());
 }
+// Heads of a wavefront: four, which share their angles and the norm's weights, once the launch fills the chip so (4096 wavefronts, four to a SIMD).  us with one and with four: prompts
+// of 36 thousand tokens, 32 and 8 heads of 128, 153.7, 142.7; 32 x 4096 tokens of 8 heads into FP4 (and back) 310, 290; 16 prompts of 60-700 tokens into FP8 9.9, 10.4.
+template <class F>
+gr_status with_heads(int64_t T, int lg, int heads, F&& f) {
+  const int64_t waves = (T + 64 / lg - 1) / (64 / lg) * heads;
+  return waves >= 4 * 4096 ? f(std::integral_constant<int, 4>()) : f(std::integral_constant<int, 1>());
+}
 template <class F>
 gr_status with_bool(bool b, F&& f) { return b ? f(std::true_type()) : f(std::false_type()); }
 
@@ -371,10 +366,13 @@ extern "C" gr_status gr_qk_norm_rope(const gr_qk_norm_rope_params* p, void* stre
   const int lg = lanes_of_head(p->d);
   const gr_status st = with_lanes(lg, [&](auto lanes) {
     return with_bool(p->pairs != 0, [&](auto pairs) {
-      const unsigned grid = grid_of(&c.t, lg, c.heads, 1);
-      if (!grid) return (gr_status)GR_ERR_UNSUPPORTED;
-      hipLaunchKernelGGL((k_qk_norm_rope<decltype(lanes)::value, decltype(pairs)::value, 1>), dim3(grid), dim3(256), 0, (hipStream_t)stream_, c);
-      return (gr_status)GR_OK;
+      return with_heads(p->T, lg, c.heads, [&](auto per_wave) {
+        constexpr int U = decltype(per_wave)::value;
+        const unsigned grid = grid_of(&c.t, lg, c.heads, U);
+        if (!grid) return (gr_status)GR_ERR_UNSUPPORTED;
+        hipLaunchKernelGGL((k_qk_norm_rope<decltype(lanes)::value, decltype(pairs)::value, U>), dim3(grid), dim3(256), 0, (hipStream_t)stream_, c);
+        return (gr_status)GR_OK;
+      });
     });
   });
   if (st) return st;
@@ -407,10 +405,13 @@ extern "C" gr_status gr_page_append(const gr_page_append_params* p, void* stream
   const gr_status st = with_lanes(lg, [&](auto lanes) {
     return with_bool(p->pairs != 0, [&](auto pairs) {
       auto go = [&](auto type) {
-        const unsigned grid = grid_of(&c.t, lg, 2 * p->Hkv, 1);
-        if (!grid) return (gr_status)GR_ERR_UNSUPPORTED;
-        hipLaunchKernelGGL((k_page_append<decltype(lanes)::value, decltype(pairs)::value, decltype(type)::value, 1>), dim3(grid), dim3(256), 0, (hipStream_t)stream_, c);
-        return (gr_status)GR_OK;
+        return with_heads(p->T, lg, 2 * p->Hkv, [&](auto per_wave) {
+          constexpr int U = decltype(per_wave)::value;
+          const unsigned grid = grid_of(&c.t, lg, 2 * p->Hkv, U);
+          if (!grid) return (gr_status)GR_ERR_UNSUPPORTED;
+          hipLaunchKernelGGL((k_page_append<decltype(lanes)::value, decltype(pairs)::value, decltype(type)::value, U>), dim3(grid), dim3(256), 0, (hipStream_t)stream_, c);
+          return (gr_status)GR_OK;
+        });
       };
       if (p->kv_type == GR_KV_BF16) return go(std::integral_constant<int, GR_KV_BF16>());
       if (p->kv_type == GR_KV_FP4) return go(std::integral_constant<int, GR_KV_FP4>());
