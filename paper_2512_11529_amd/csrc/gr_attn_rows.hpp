@@ -3,6 +3,7 @@
 #pragma once
 #include <type_traits>
 #include "gr_attn_tile.hpp"
+#include "gr_pages.hpp"
 
 namespace {
 

@@ -96,34 +96,77 @@ constexpr PagedCost kPagedCost[2][2] = {      // [head size 128][FP8]; rate in b
     {{3.3, 1.5, 1.2, 2.0, 2.0, 1.05, 0.95, 1.5, 0.7, 3.1, 8.0e6}, {3.3, 1.5, 1.4, 2.0, 2.0, 1.05, 0.95, 1.5, 0.8, 3.1, 4.0e6}},
     {{0.7, 0.15, 1.9, 1.95, 2.1, 0.9, 1.25, 0.4, 0.9, 1.95, 7.9e6}, {1.5, 2.35, 2.05, 1.6, 4.0, 1.45, 1.35, 1.25, 0.9, 2.2, 5.4e6}}};
 
-// FP4: blocks of 16 rows where there are no more, else of 32, and segments for about four workgroups to a CU.
+// FP4, up to 80 rows of a pair: the same choice by estimated time, over blocks of 16 rows (32 for more than 16) with four or, ks = 2, eight wavefronts, blocks of 128 for more than 24, and the
+// prefix packed.  few16 and few32 are a block's fixed time and their steps those of 128 tokens for four wavefronts (`eight` more, and half the steps, for eight), per_cu such
+// blocks of four wavefronts share a CU.  Fitted to 9170 random calls of 1 to 128 requests of 10 to 16384 tokens with 1 to 80 rows, half of them behind a prefix of 64 to 8192 tokens, each timed in up to 50 ways:
+// with them the mean call takes 1.026 times the best of its ways, one in twenty more than 1.15 (1.05 and 1.25 without a join's time for each segment: 32 of them for 2000 tokens), the worst 1.6: a few rows of ragged or very long lists left in one segment.
+struct Fp4Cost { double start, few16, step16, per_cu16, few32, step32, per_cu32, eight, unit, tile1, tile2, shared, shared_tile, join, join_one, rate; };      // join_one: for each segment
+constexpr Fp4Cost kFp4Cost[2] = {{3.84, 1.55, 0.63, 2.66, 1.76, 0.74, 1.56, 0.39, 1.54, 1.03, 0.99, 1.15, 0.75, 1.5, 0.25, 5.9e6},
+                                 {4.85, 1.63, 0.74, 1.68, 2.47, 1.01, 1.53, 0.51, 2.17, 1.47, 1.36, 0.83, 1.13, 1.5, 0.1, 4.7e6}};
 PagedPlan plan_fp4(const gr_attn_paged_params* p) {
   PagedPlan plan{};
-  const int64_t M = (int64_t)p->W * (p->Hq / p->Hkv), list = (int64_t)p->prefix_L + p->max_L;
-  plan.rows = M <= 16 ? 16 : 32;
-  const int64_t blocks = (int64_t)p->B * p->Hkv * ((M + plan.rows - 1) / plan.rows), most = list / 256;
-  int64_t n = 1024 / blocks;
-  n = n < most ? n : most;
-  plan.ns[1] = (int)(n < 1 ? 1 : n > 64 ? 64 : n);
-  plan.ks = 1;
+  const int64_t M = (int64_t)p->W * (p->Hq / p->Hkv), all = p->B * M, pairs = (int64_t)p->B * p->Hkv, list = (int64_t)p->prefix_L + p->max_L;
+  const Fp4Cost& c = kFp4Cost[p->d == 128];
+  const int rows = M <= 16 ? 16 : 32;
+  const double few0 = rows == 16 ? c.few16 : c.few32, step = rows == 16 ? c.step16 : c.step32, per_cu = rows == 16 ? c.per_cu16 : c.per_cu32;
+  const double partial_us = 2.0 * p->B * p->W * p->Hq * p->d * 4 / 2.7e6, token_bytes = 17.0 / 16 * p->Hkv * p->d;
+  auto parts = [](int64_t n, int64_t of) { return (n + of - 1) / of; };
+  auto larger = [](double a, double b) { return a > b ? a : b; };
+  auto both = [](double a, double b) { return sqrt(sqrt(a * a * a * a + b * b * b * b)); };
+  double least = 0;
+  auto look_at = [&](int r, int n0, int n1, int ks, double us) {
+    const int n = n0 + n1;
+    us += n > 1 ? c.join + (c.join_one + partial_us) * n : 0.0;
+    if (plan.rows && !(us < least)) return;
+    least = us;
+    plan.rows = r; plan.ns[0] = n0; plan.ns[1] = n1; plan.ks = ks;
+  };
+  const double list_us = list * p->B * token_bytes / c.rate;
+  for (const int n : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
+    if (n > 1 && n * 64 > list) break;
+    const double tiles = (double)parts(parts(list, n), KT), blocks = (double)(parts(pairs * n, 8) * parts(M, rows));
+    for (const int ks : {1, 2}) {
+      const double few = few0 + step * tiles / (2 * ks) + (ks == 2 ? c.eight : 0.0);
+      look_at(rows, 0, n, ks, both(few * larger(1.0, blocks * ks / (32 * per_cu)), list_us));
+    }
+    if (M <= 24 || n > 16) continue;
+    const int64_t on_xcd = parts(pairs * n, 8);
+    const bool sets = list > KT && pairs * n <= 256;
+    const double unit = sets ? (c.unit + c.tile2 * (double)(((int64_t)tiles + 1) >> 1)) * (double)parts(on_xcd, 32) : (c.unit + c.tile1 * tiles) * larger(1.0, on_xcd / 64.0);
+    look_at(128, 0, n, sets ? 2 : 1, both(unit, list_us));
+  }
+  // packed, as the beams of one request (offsets inside its rows fit 32 bits)
+  if (p->prefix_L > 0 && p->B > 1 && all < ((int64_t)1 << 22) && all * p->Hkv * p->d < ((int64_t)1 << 31)) {
+    const double packed_us = (p->prefix_L + (double)p->max_L * p->B) * token_bytes / c.rate;
+    for (const int n0 : {1, 2, 3, 4, 6, 8, 12, 16}) {
+      if (n0 > 1 && n0 * 96 > p->prefix_L) break;
+      const double shared = c.shared + c.shared_tile * (double)parts(parts(p->prefix_L, n0), KT), shared_blocks = (double)(parts((int64_t)p->Hkv * n0, 8) * parts(all, 128));
+      for (const int n1 : {1, 2, 4}) {
+        if (n1 > 1 && n1 * 128 > p->max_L) break;
+        const double few = few0 + step * (double)parts(parts(p->max_L, n1), KT) / 2, few_blocks = (double)(parts(pairs * n1, 8) * parts(M, rows));
+        look_at(rows, n0, n1, 1, both(larger(larger(few, shared), (shared * shared_blocks + few * few_blocks * 2 / per_cu) / 64), packed_us));
+      }
+    }
+  }
+  plan.find = plan.rows == 128 && plan.ks == 1 && pairs * plan.ns[1] > 256 && p->B >= 2 && p->B <= kRankB;
   return plan;
 }
 
 PagedPlan plan_paged(const gr_attn_paged_params* p) {
-  if (p->kv_type == GR_KV_FP4) return plan_fp4(p);
   PagedPlan plan{};
   const int64_t g = p->Hq / p->Hkv, M = p->W * g, all = p->B * M, pairs = (int64_t)p->B * p->Hkv;
-  const bool kv8 = p->kv_type == GR_KV_FP8;
+  const bool kv8 = p->kv_type == GR_KV_FP8, kv4 = p->kv_type == GR_KV_FP4;
   auto parts = [](int64_t n, int64_t of) { return (n + of - 1) / of; };
   if (M > 80) {
     gr_attn_params q{};
     q.B = p->B; q.W = p->W; q.Hq = p->Hq; q.Hkv = p->Hkv; q.d = p->d; q.max_L = p->prefix_L + p->max_L;
     q.total_L = (int64_t)q.B * q.max_L;                      // (the lengths are on the GPU)
-    const AttnPlan a = plan_attn(&q, kv8);
+    const AttnPlan a = plan_attn(&q, kv8 || kv4);
     plan.rows = a.mwg; plan.ns[1] = a.nsplit; plan.ks = a.ks;
     plan.find = a.many && a.ks == 1 && p->B >= 2 && p->B <= kRankB;
     return plan;
   }
+  if (kv4) return plan_fp4(p);
   const PagedCost& c = kPagedCost[p->d == 128][kv8];
   const double partial_us = 2.0 * p->B * p->W * p->Hq * p->d * 4 / 2.7e6, token_bytes = 2.0 * p->Hkv * p->d * (kv8 ? 1 : 2);
   constexpr int kCounts[] = {1, 2, 3, 4, 6, 8, 12, 16};

@@ -5,13 +5,14 @@
 //   - K never meets LDS.  Lane (token t, quarter h) of a wavefront takes the quarter of its token's head that lies in one piece, 16 or 8 bytes under one scale.  The sum over the
 //     head's elements may be made in any order, so a matrix instruction's k-th step takes the eight codes of each quarter's k-th word, and Q is held in the same order.
 //   - V has to be transposed: its operand holds eight tokens of one element.  It is widened into LDS rows and read from there with ds_read_b64_tr_b16.
+#define GR_ROWS_FP4
 #include "gr_paged.hpp"
 
 namespace {
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
-// 16 * NB rows of a (request, KV head) pair against a segment of its keys.  The four wavefronts hold the same rows and take every fourth 32 tokens each; nobody waits for
+// 16 * NB rows of a (request, KV head) pair against a segment of its keys.  The wavefronts hold the same rows and take 32 tokens each in turn; nobody waits for
 // anybody until their (maximum, sum, O) are joined in LDS.
 // Bound: memory (17/32 byte an element).
 template <int D>
@@ -26,9 +27,9 @@ struct Fp4 {
   // 16-byte pieces of a V row stand permuted, piece p of row r in slot p ^ swz(r): the eight rows that 32 lanes read 32 bytes each of are then in different banks
   static __device__ __forceinline__ int swz(int r) { return D == 128 ? 2 * (r & 7) : 2 * ((r >> 1) & 3); }
 };
-constexpr int fp4_few_lds_bytes(int d, int nb) { return 4 * 32 * d * 2 + 4 * 16 * nb * 8; }
+constexpr int fp4_few_lds_bytes(int d, int nb, int waves) { return waves * (32 * d * 2 + 16 * nb * 8); }
 
-template <int D, int NB, int ARG>
+template <int D, int NB, int WAVES, int ARG>
 __device__ __forceinline__ void few_rows4(const AttnCtx& c, const unsigned id) {
   using F = Fp4<D>;
   constexpr int FT = F::FT, NV = F::NV, NW = F::NW, KS = F::KS, DB = F::DB, ROWS = 16 * NB;
@@ -71,17 +72,18 @@ __device__ __forceinline__ void few_rows4(const AttnCtx& c, const unsigned id) {
   if (sp > 0) { window = seg0 >> c.shift; numbers = numbers_from(window); }
   int ahead = numbers_from(window + 64);
 
-  // ---- a tile of codes in registers
-  struct Tile { typename F::words k[2], v[2]; uint32_t ks[2], vs[2]; };
+  // ---- a tile's codes and powers in registers: halves of 16 tokens, each of which lies in one page
+  struct Codes { typename F::words w[2]; uint32_t power[2]; };
   const uint32_t ps = 1u << c.shift, codes = gr_fp4_codes(ps, D), record = gr_fp4_record(ps, D);
   const uint8_t* k_head = (const uint8_t*)c.ks + (size_t)kvh * record;
   const uint8_t* v_head = (const uint8_t*)c.vs + (size_t)kvh * record;
-  const size_t page_bytes = (size_t)record * (unsigned)c.Hkv;
-  const uint32_t k_off = (uint32_t)(n16 * (D / 2) + h * (NV / 2)), ks_off = (uint32_t)(n16 * (D / 32) + h * NV / 32);
+  const uint32_t page_bytes = record * (unsigned)c.Hkv;
+  const uint32_t k_off = (uint32_t)(n16 * (D / 2) + h * (NV / 2)), kp_off = (uint32_t)(n16 * (D / 32) + h * NV / 32);
   const int vr = lane >> 2, vb = lane & 3;                   // V: lane (token vr, quarter vb)
-  const uint32_t v_off = (uint32_t)(lane * (NV / 2)), vs_off = (uint32_t)(vr * (D / 32) + vb * NV / 32);
-  auto load = [&](int j) {
-    Tile t;
+  const uint32_t v_off = (uint32_t)(lane * (NV / 2)), vp_off = (uint32_t)(vr * (D / 32) + vb * NV / 32);
+  size_t page_at[2];                                         // of the tile asked for last
+  uint32_t in_at[2];
+  auto locate = [&](int j) {
 #pragma unroll
     for (int i = 0; i < 2; i++) {
       const int tok = seg0 + j * FT + 16 * i, p = tok >> c.shift;
@@ -90,16 +92,17 @@ __device__ __forceinline__ void few_rows4(const AttnCtx& c, const unsigned id) {
         numbers = ahead;
         ahead = numbers_from(window + 64);
       }
-      const size_t at = (size_t)(unsigned)__builtin_amdgcn_readlane(numbers, p - window) * page_bytes;
-      const uint32_t in = (uint32_t)tok & (ps - 1);
-      const uint8_t* kp = k_head + at + in * (D / 2);
-      const uint8_t* vp = v_head + at + in * (D / 2);
-      const uint8_t* kq = k_head + at + codes + in * (D / 32);
-      const uint8_t* vq = v_head + at + codes + in * (D / 32);
-      t.k[i] = *(const typename F::words*)(kp + k_off);
-      t.ks[i] = kq[ks_off];
-      t.v[i] = *(const typename F::words*)(vp + v_off);
-      t.vs[i] = vq[vs_off];
+      page_at[i] = (size_t)(unsigned)__builtin_amdgcn_readlane(numbers, p - window) * page_bytes;
+      in_at[i] = (uint32_t)tok & (ps - 1);
+    }
+  };
+  auto load = [&](const uint8_t* head, uint32_t off, uint32_t power_off) {
+    Codes t;
+#pragma unroll
+    for (int i = 0; i < 2; i++) {
+      const uint8_t* page = head + page_at[i];
+      t.w[i] = *(const typename F::words*)(page + in_at[i] * (D / 2) + off);
+      t.power[i] = *(page + codes + in_at[i] * (D / 32) + power_off);
     }
     return t;
   };
@@ -114,13 +117,12 @@ __device__ __forceinline__ void few_rows4(const AttnCtx& c, const unsigned id) {
   }
   uint16_t* mine = smem + wave * F::PLACE;
   const int lds_v = (int)(uintptr_t)(__attribute__((address_space(3))) uint16_t*)mine;
-  int w_at[NW / 2], r_at[DB];                                // byte addresses of the lane's writes (two pieces each) and reads, of the first half
+  int w_at[NW / 2], r_at;                                    // byte addresses of the lane's writes (two pieces each) and reads, of the first half
 #pragma unroll
   for (int i = 0; i < NW / 2; i++) w_at[i] = lds_v + vr * (D * 2) + (((NW * vb + 2 * i) ^ F::swz(vr)) << 4);
   {
     const int row = 4 * h + (n16 >> 2);
-#pragma unroll
-    for (int db = 0; db < DB; db++) r_at[db] = lds_v + row * (D * 2) + (((2 * db) ^ F::swz(row)) << 4) + ((n16 & 3) << 3);
+    r_at = lds_v + row * (D * 2) + (F::swz(row) << 4) + ((n16 & 3) << 3);       // (32 elements on: another 32 bytes, in the swizzle's order)
   }
   typedef u32x4 __attribute__((address_space(3))) * lds_u32x4;
   typedef s16x4 __attribute__((address_space(3))) * lds_s16x4;
@@ -167,11 +169,12 @@ __device__ __forceinline__ void few_rows4(const AttnCtx& c, const unsigned id) {
         }
     }
     bring_v();
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
     for (int db = 0; db < DB; db++) {
       typedef short s16x8 __attribute__((ext_vector_type(8)));
-      const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)(uint32_t)r_at[db]);
-      const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)(uint32_t)(r_at[db] + 16 * D * 2));
+      const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)(uint32_t)(r_at ^ (32 * db)));
+      const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)(uint32_t)((r_at ^ (32 * db)) + 16 * D * 2));
       const bf16x8 v = __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
       for (int nb = 0; nb < NB; nb++) o[db][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[nb], o[db][nb], 0, 0, 0);
@@ -179,11 +182,12 @@ __device__ __forceinline__ void few_rows4(const AttnCtx& c, const unsigned id) {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // (LDS serves a wavefront in order: the next tile's V goes where this one's was)
   };
 
-  // ---- the beams' own tokens first: their addresses need no page numbers
+  // ---- the beams' own tokens, while the first tile is on its way
   const uint32_t own_bytes = (uint32_t)c.Hkv * D * 2;
   const char* ku_b = (const char*)(c.ku + ((size_t)bu * (unsigned)(c.W * c.ND) * (unsigned)c.Hkv + kvh) * D);
   const char* vu_b = (const char*)(c.vu + ((size_t)bu * (unsigned)(c.W * c.ND) * (unsigned)c.Hkv + kvh) * D);
-  for (int oj = wave; oj < n_own; oj += 4) {
+  auto own_tokens = [&]() __attribute__((always_inline)) {
+  for (int oj = wave; oj < n_own; oj += WAVES) {
     uint32_t off[2];                                         // of row 16 i + n16 of the tile
 #pragma unroll
     for (int i = 0; i < 2; i++) {
@@ -198,15 +202,20 @@ __device__ __forceinline__ void few_rows4(const AttnCtx& c, const unsigned id) {
       off[i] = (uint32_t)prow * own_bytes;
     }
     f32x4 s[2][NB];
-    u32x4 v[2][NW];
+#pragma unroll
+    for (int i = 0; i < 2; i++) {
+      const char* vrow = vu_b + (uint32_t)__shfl((int)off[i], vr, 64) + vb * NW * 16;
+      u32x4 v[NW];
+#pragma unroll
+      for (int w = 0; w < NW; w++) v[w] = *(const u32x4*)(vrow + w * 16);
+#pragma unroll
+      for (int w = 0; w < NW; w++) put_v(i, w, v[w]);
+    }
 #pragma unroll
     for (int i = 0; i < 2; i++) {
       bf16x8 k[KS];
 #pragma unroll
       for (int st = 0; st < KS; st++) k[st] = *(const bf16x8*)(ku_b + off[i] + h * NV * 2 + 16 * st);
-      const char* vrow = vu_b + (uint32_t)__shfl((int)off[i], vr, 64);
-#pragma unroll
-      for (int w = 0; w < NW; w++) v[i][w] = *(const u32x4*)(vrow + (vb * NW + w) * 16);
 #pragma unroll
       for (int nb = 0; nb < NB; nb++) {
         s[i][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -218,30 +227,22 @@ __device__ __forceinline__ void few_rows4(const AttnCtx& c, const unsigned id) {
     unsigned n[NB];
 #pragma unroll
     for (int nb = 0; nb < NB; nb++) { lo[nb] = (beam_q[nb] - beam0) * c.u - oj * FT; n[nb] = qrow[nb] >= 0 ? (unsigned)c.u : 0u; }
-    softmax_pv(s, lo, n, false, [&] {
-#pragma unroll
-      for (int i = 0; i < 2; i++)
-#pragma unroll
-        for (int w = 0; w < NW; w++) put_v(i, w, v[i][w]);
-    });
+    softmax_pv(s, lo, n, false, [] {});
   }
+  };
 
-  // ---- the list: the next tile is on its way while one is taken
-  const int first = (wave + 4 - (n_own & 3)) & 3;            // (the wavefronts behind those with own tokens begin)
-  Tile t;
-  if (first < nt) t = load(first);
-  for (int j = first; j < nt; j += 4) {
-    Tile now = t;
-    if (j + 4 < nt) t = load(j + 4);
+  // ---- the list: a tile's K is asked for when the one before has been multiplied, its V when that one is in LDS
+  int j = (wave + WAVES - (n_own & (WAVES - 1))) & (WAVES - 1);                      // (the wavefronts behind those with own tokens begin)
+  Codes k, v;
+  if (j < nt) {
+    locate(j);
+    k = load(k_head, k_off, kp_off);
+    v = load(v_head, v_off, vp_off);
+  }
+  own_tokens();
+  for (; j < nt; j += WAVES) {
     const int left = seg1 - (seg0 + j * FT);
-    const bool all = left >= FT;
-    if (!all) {                                              // rows behind the list hold anything: V's must not be infinite times 0
-#pragma unroll
-      for (int i = 0; i < 2; i++) {
-        const bool there = 16 * i + vr < left;
-        now.vs[i] = there ? now.vs[i] : 127u;
-      }
-    }
+    const bool all = left >= FT, more = j + WAVES < nt;
     f32x4 s[2][NB];
 #pragma unroll
     for (int i = 0; i < 2; i++) {
@@ -249,10 +250,14 @@ __device__ __forceinline__ void few_rows4(const AttnCtx& c, const unsigned id) {
       for (int nb = 0; nb < NB; nb++) s[i][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int st = 0; st < KS; st++) {
-        const bf16x8 k = __builtin_bit_cast(bf16x8, fp4_values8(now.k[i][st], now.ks[i]));
+        const bf16x8 x = __builtin_bit_cast(bf16x8, fp4_values8(k.w[i][st], k.power[i]));
 #pragma unroll
-        for (int nb = 0; nb < NB; nb++) s[i][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[nb][st], s[i][nb], 0, 0, 0);
+        for (int nb = 0; nb < NB; nb++) s[i][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, q[nb][st], s[i][nb], 0, 0, 0);
       }
+    }
+    if (more) {
+      locate(j + WAVES);
+      k = load(k_head, k_off, kp_off);
     }
     int lo[NB];
     unsigned n[NB];
@@ -260,14 +265,18 @@ __device__ __forceinline__ void few_rows4(const AttnCtx& c, const unsigned id) {
     for (int nb = 0; nb < NB; nb++) { lo[nb] = 0; n[nb] = (unsigned)left; }
     softmax_pv(s, lo, n, all, [&] {
 #pragma unroll
-      for (int i = 0; i < 2; i++)
+      for (int i = 0; i < 2; i++) {
+        // (rows behind the list hold anything, and must not be infinite times 0)
+        const uint32_t power = all || 16 * i + vr < left ? v.power[i] : 127u;
 #pragma unroll
-        for (int w = 0; w < NW; w++) put_v(i, w, __builtin_bit_cast(u32x4, fp4_values8(now.v[i][w], now.vs[i])));
+        for (int w = 0; w < NW; w++) put_v(i, w, __builtin_bit_cast(u32x4, fp4_values8(v.w[i][w], power)));
+      }
+      if (more) v = load(v_head, v_off, vp_off);
     });
   }
 
-  // ---- the four wavefronts' parts join in LDS, 16 rows at a time; then every one has columns of its own to write
-  f32x2* s_ml = (f32x2*)(smem + 4 * F::PLACE);
+  // ---- the wavefronts' parts join in LDS, 16 rows at a time; then every one has columns of its own to write
+  f32x2* s_ml = (f32x2*)(smem + WAVES * F::PLACE);
 #pragma unroll
   for (int nb = 0; nb < NB; nb++) {
     float l = l_run[nb] + __shfl_xor(l_run[nb], 16, 64);
@@ -283,11 +292,11 @@ __device__ __forceinline__ void few_rows4(const AttnCtx& c, const unsigned id) {
     for (int db = 0; db < DB; db++) to[64 * db] = o[db][nb];
     __syncthreads();
     if (qrow[nb] < 0) continue;
-    float top = -INFINITY, l = 0.f, a[4];
+    float top = -INFINITY, l = 0.f, a[WAVES];
 #pragma unroll
-    for (int w = 0; w < 4; w++) top = fmaxf(top, s_ml[(w * NB + nb) * 16 + n16].x);
+    for (int w = 0; w < WAVES; w++) top = fmaxf(top, s_ml[(w * NB + nb) * 16 + n16].x);
 #pragma unroll
-    for (int w = 0; w < 4; w++) {
+    for (int w = 0; w < WAVES; w++) {
       const f32x2 ml = s_ml[(w * NB + nb) * 16 + n16];
       a[w] = ml.x > -INFINITY ? __builtin_amdgcn_exp2f(ml.x - top) : 0.f;
       l += ml.y * a[w];
@@ -297,11 +306,12 @@ __device__ __forceinline__ void few_rows4(const AttnCtx& c, const unsigned id) {
     const int left = min(32, M - (row_w & ~31)), r32 = (row_w & 31) + 16 * nb + n16;
     const size_t row_p = (((size_t)bu * (unsigned)ns + (unsigned)sp) * (unsigned)late->Hkv + kvh) * (unsigned)M + (unsigned)(row_w & ~31);
 #pragma unroll
-    for (int k = 0; k < DB / 4; k++) {
-      const int db = wave * (DB / 4) + k;
+    for (int k = 0; k < (DB + WAVES - 1) / WAVES; k++) {
+      const int db = wave + k * WAVES;
+      if (DB < WAVES && db >= DB) break;
       f32x4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int w = 0; w < 4; w++) {
+      for (int w = 0; w < WAVES; w++) {
         const f32x4 y = *((const f32x4*)(smem + w * F::PLACE) + 64 * db + lane);
 #pragma unroll
         for (int e = 0; e < 4; e++) x[e] += y[e] * a[w];
@@ -322,20 +332,55 @@ __device__ __forceinline__ void few_rows4(const AttnCtx& c, const unsigned id) {
   }
 }
 
+template <int D, int NB, int WAVES>
+__global__ void __launch_bounds__(WAVES * 64) __attribute__((amdgpu_waves_per_eu(2))) k_fp4_few(AttnCtx c) {
+  few_rows4<D, NB, WAVES, 0>(c, blockIdx.x);
+}
+
+// Blocks of 128 and 256 rows: gr_beam_attn's body.
+template <int D, int NWAVES, int KS, bool FIND>
+__global__ void __launch_bounds__(NWAVES * 64 * KS) __attribute__((amdgpu_waves_per_eu(2, 2))) k_fp4_attn(AttnCtx c) {
+  constexpr int NCB = 1;
+  constexpr bool CAUSAL = false, PAGED = true, KV8 = true, WHOLE = true;
+#include "gr_attn_rows.inc"
+}
+
+
+// A packed prefix by blocks of 128 rows of all requests, which are dealt first (arguments c), and each request's list by blocks of 16 or 32 (arguments few).
+constexpr int fp4_mix_lds_bytes(int d, int nb) { return attn_lds_bytes(d, 128, 1) > fp4_few_lds_bytes(d, nb, 4) ? attn_lds_bytes(d, 128, 1) : fp4_few_lds_bytes(d, nb, 4); }
 template <int D, int NB>
-__global__ void __launch_bounds__(256) k_fp4_few(AttnCtx c) {
-  few_rows4<D, NB, 0>(c, blockIdx.x);
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) k_fp4_mix(AttnCtx c, AttnCtx few, unsigned blocks0) {
+  if (blockIdx.x >= blocks0) {
+    few_rows4<D, NB, 4, 1>(few, blockIdx.x - blocks0);
+    return;
+  }
+  constexpr int NCB = 1, NWAVES = 4, KS = 1;
+  constexpr bool CAUSAL = false, FIND = false, PAGED = true, KV8 = true, WHOLE = true;
+#include "gr_attn_rows.inc"
 }
 
 }  // namespace
 
 gr_status gr_paged_fp4(const gr_attn_paged_params* p, void* workspace, size_t workspace_bytes, hipStream_t stream) {
-  return run_paged(p, workspace, workspace_bytes, stream, [&](const PagedPlan& plan, const AttnCtx&, const AttnCtx& c, unsigned grid, unsigned) -> gr_status {
-    auto few = [&](auto dim) -> gr_status {
-      constexpr int D = decltype(dim)::value;
-      if (plan.rows == 16) return launch<k_fp4_few<D, 1>>(fp4_few_lds_bytes(D, 1), 256, grid, stream, c);
-      return launch<k_fp4_few<D, 2>>(fp4_few_lds_bytes(D, 2), 256, grid, stream, c);
+  return run_paged(p, workspace, workspace_bytes, stream, [&](const PagedPlan& plan, const AttnCtx& c0, const AttnCtx& c, unsigned grid, unsigned blocks0) -> gr_status {
+    auto few = [&](auto dim, auto blocks) -> gr_status {
+      constexpr int D = decltype(dim)::value, NB = decltype(blocks)::value;
+      if (plan.ns[0] > 0) return launch<k_fp4_mix<D, NB>>(fp4_mix_lds_bytes(D, NB), 256, grid, stream, c0, c, blocks0);
+      if (plan.ks == 2) return launch<k_fp4_few<D, NB, 8>>(fp4_few_lds_bytes(D, NB, 8), 512, grid, stream, c);
+      return launch<k_fp4_few<D, NB, 4>>(fp4_few_lds_bytes(D, NB, 4), 256, grid, stream, c);
     };
-    return p->d == 128 ? few(std::integral_constant<int, 128>()) : few(std::integral_constant<int, 64>());
+    auto rows = [&](auto dim) -> gr_status {
+      constexpr int D = decltype(dim)::value;
+      if (plan.rows == 16) return few(dim, std::integral_constant<int, 1>());
+      if (plan.rows == 32) return few(dim, std::integral_constant<int, 2>());
+      if (plan.ks == 2) return launch<k_fp4_attn<D, 4, 2, false>>(attn_lds_bytes(D, 128, 2), 512, grid, stream, c);
+      if (plan.rows == 128) {
+        if (plan.find) return launch<k_fp4_attn<D, 4, 1, true>>(attn_lds_bytes(D, 128, 1), 256, grid, stream, c);
+        return launch<k_fp4_attn<D, 4, 1, false>>(attn_lds_bytes(D, 128, 1), 256, grid, stream, c);
+      }
+      if (plan.find) return launch<k_fp4_attn<D, 8, 1, true>>(attn_lds_bytes(D, 256, 1), 512, grid, stream, c);
+      return launch<k_fp4_attn<D, 8, 1, false>>(attn_lds_bytes(D, 256, 1), 512, grid, stream, c);
+    };
+    return p->d == 128 ? rows(std::integral_constant<int, 128>()) : rows(std::integral_constant<int, 64>());
   });
 }
