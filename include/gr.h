@@ -388,7 +388,7 @@ gr_status gr_page_write(const gr_page_write_params* p, void* stream);
 
 /* gr_page_append - gr_page_write for the rows of a projection: the keys are normed and rotated on the way, as gr_qk_norm_rope does it (k_weight NULL: not normed; rot 0: not
  * rotated), in fp32 and rounded once, to the pool's type.  Values go as they are.  Rows whose slot is outside [0, n_pages * page_size) or, with rot > 0, whose position is outside
- * [0, n_pos) are not written; a slot that two rows have holds either's elements, in parts too.  GR_KV_FP8: codes as gr_page_write makes them (of rotated or normed keys the quotient
+ * [0, n_pos) are not written; a slot that two rows have holds either's elements, in parts too (GR_KV_FP4: codes of one may stand under scales of the other).  GR_KV_FP8: codes as gr_page_write makes them (of rotated or normed keys the quotient
  * may be one unit of fp32 off the division's).  GR_KV_FP4: a block's scale is the smallest power of two, from 2^-120 to 2^125, with |x| <= 7 * scale for its 32 values (no value is
  * further off than half the distance of the codes around it); codes are the nearest, ties to even.  Only enqueues on `stream`.  The pools do not overlap k, v or each other.
  * Supported: d a multiple of 16 (GR_KV_FP4: 32) up to 256; rot a multiple of 16 up to d; Hkv * d at most 2^20; the strides multiples of 8; T and n_pages * page_size below

@@ -88,6 +88,32 @@ def test_parts_of_fused_rows_in_place_and_into_own_caches(Hq, Hkv, d, rot, pairs
         assert torch.equal(got[~skip], w[~skip]) and torch.equal(got[skip], b[skip])
 
 
+def test_values_beside_queries_alone():
+    g = torch.Generator().manual_seed(8)
+    q, v = inputs(g, 21, 3, 96).to(DEV), inputs(g, 21, 2, 96).to(DEV)
+    table, pos = table_of(N_POS, 32).to(DEV), torch.randint(0, N_POS, (21,), generator=g).int().to(DEV)
+    v_out = torch.zeros_like(v)
+    got, none = gr.gr_qk_norm_rope(q, None, pos, table, v=v, v_out=v_out)
+    assert none is None and torch.equal(v_out, v) and torch.equal(got, gr.gr_qk_norm_rope(q, None, pos, table)[0])
+
+
+@pytest.mark.parametrize("T", [4096, 20000])
+def test_many_rows_are_made_as_few_are(T):
+    """Launches of four heads a wavefront and of one give the same bits."""
+    g = torch.Generator().manual_seed(T)
+    rows = inputs(g, T, 40, 128).to(DEV)
+    q, k = rows[:, :32], rows[:, 32:]
+    table, pos = table_of(N_POS, 128).to(DEV), torch.randint(0, N_POS, (T,), generator=g).int().to(DEV)
+    qw, kw = (1 + 0.3 * torch.randn((128,), generator=g).to(DEV) for _ in range(2))
+    for pairs in (False, True):
+        all_q, all_k = gr.gr_qk_norm_rope(q, k, pos, table, qw, kw, pairs=pairs)
+        for at in (0, 77, T - 33):
+            some = slice(at, at + 33)
+            few = gr.gr_qk_norm_rope(q[some], k[some], pos[some], table, qw, kw, pairs=pairs)
+            assert torch.equal(all_q[some], few[0]) and torch.equal(all_k[some], few[1])
+        check(all_q[-8:].cpu(), q[-8:].cpu(), qw.cpu(), 1e-6, pos[-8:].cpu(), table.cpu(), pairs)
+
+
 def test_zeros_infinities_and_nan_stay_in_their_heads():
     T, d = 6, 128
     x = torch.ones((T, 2, d), dtype=torch.bfloat16)

@@ -4,7 +4,7 @@ import ctypes
 import pytest
 import torch
 
-from test_paged_refusals import A, F, I, INF, L, NAN, P, gr, struct  # noqa: F401  (gr: the fixture)
+from test_paged_refusals import A, ATTN, F, GOOD_ATTN, GOOD_WRITE, I, INF, L, NAN, P, WRITE, gr, struct  # noqa: F401  (gr: the fixture)
 
 ROPE = struct((L, "T"), (I, "Hq Hkv d rot pairs n_pos"), (F, "eps"), (L, "q_stride k_stride v_stride q_out_stride k_out_stride v_out_stride"),
               (P, "q k v q_weight k_weight table pos q_out k_out v_out"))
@@ -78,3 +78,26 @@ def test_tensors_off_the_gpu_are_refused(gr):  # noqa: F811
         gr.gr_page_append(b, b, i, pool, pool)
     with pytest.raises(TypeError, match="k: expected a CUDA tensor"):
         gr.gr_page_read(pool, pool, i, b, b)
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(B=0), -1), (dict(Hkv=3), -1), (dict(u=4), -1), (dict(max_L=-1), -1), (dict(n_pages=0), -1), (dict(kv_type=3), -1), (dict(sm_scale=INF), -1), (dict(q=None), -1), (dict(k_pages=None), -1),
+    (dict(prefix_pages=None), -1), (dict(block_table=None), -1), (dict(seq_lens=None), -1), (dict(k_unshared=None), -1), (dict(max_L=129), -1), (dict(k_pages=A + 8), -1), (dict(lse_out=A + 1), -1),
+    (dict(d=96), -2), (dict(d=32), -2), (dict(page_size=8, max_pages=16), -2), (dict(page_size=48), -2), (dict(prefix_L=24), -2), (dict(n_pages=2 ** 27), -2), (dict(Hkv=2048, Hq=2048), -2), (dict(W=2 ** 21), -2),
+    (dict(page_size=1024, max_pages=2 ** 20, max_L=2 ** 30 - 1024, prefix_L=1024), -2), (dict(B=1 << 21, W=1, Hq=8, Hkv=8, prefix_L=0), -2), (dict(B=1 << 14, W=1 << 14, Hq=8, Hkv=8), -2)])
+def test_attention_over_fp4_pages(gr, change, status):  # noqa: F811
+    p = ATTN(**{**GOOD_ATTN, "kv_type": 2, "k_scale": NAN, "v_scale": 0.0, **change})          # (scales of FP8 are not looked at)
+    assert gr.load_library().gr_beam_attn_paged(ctypes.byref(p), A, 1 << 40, None) == status
+
+
+def test_workspace_of_attention_over_fp4_pages(gr):  # noqa: F811
+    lib, p = gr.load_library(), ATTN(**{**GOOD_ATTN, "kv_type": 2, "prefix_L": 4096, "max_L": 100})
+    need = lib.gr_beam_attn_paged_workspace_bytes(ctypes.byref(p))
+    assert need > 0
+    assert lib.gr_beam_attn_paged(ctypes.byref(p), None, need, None) == -1
+    assert lib.gr_beam_attn_paged(ctypes.byref(p), A + 128, need, None) == -1
+    assert lib.gr_beam_attn_paged(ctypes.byref(p), A, need - 1, None) == -3
+
+
+def test_the_plain_write_has_no_fp4(gr):  # noqa: F811
+    assert gr.load_library().gr_page_write(ctypes.byref(WRITE(**{**GOOD_WRITE, "kv_type": 2})), None) == -1
