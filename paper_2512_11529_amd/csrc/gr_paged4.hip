@@ -128,8 +128,8 @@ __device__ __forceinline__ void few_rows4(const AttnCtx& c, const unsigned id) {
   typedef s16x4 __attribute__((address_space(3))) * lds_s16x4;
   auto put_v = [&](int i, int piece, u32x4 x) { *(lds_u32x4)(uintptr_t)(uint32_t)(w_at[piece / 2] + 16 * D * 2 * i + 16 * (piece & 1)) = x; };
 
-  // The tile's scores to probabilities and onto O, once V is in LDS.  rows [lo, lo + n) of the tile are seen by the column.
-  auto softmax_pv = [&](f32x4 (&s)[2][NB], const int (&lo)[NB], const unsigned (&n)[NB], bool all, auto&& bring_v) __attribute__((always_inline)) {
+  // The tile's scores to probabilities and onto O; V is in LDS.  rows [lo, lo + n) of the tile are seen by the column.
+  auto softmax_pv = [&](f32x4 (&s)[2][NB], const int (&lo)[NB], const unsigned (&n)[NB], bool all) __attribute__((always_inline)) {
     bf16x8 p[NB];
 #pragma unroll
     for (int nb = 0; nb < NB; nb++) {
@@ -168,8 +168,6 @@ __device__ __forceinline__ void few_rows4(const AttnCtx& c, const unsigned id) {
           p[nb][4 * i + e] = (__bf16)x;
         }
     }
-    bring_v();
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
     for (int db = 0; db < DB; db++) {
       typedef short s16x8 __attribute__((ext_vector_type(8)));
@@ -211,6 +209,7 @@ __device__ __forceinline__ void few_rows4(const AttnCtx& c, const unsigned id) {
 #pragma unroll
       for (int w = 0; w < NW; w++) put_v(i, w, v[w]);
     }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
     for (int i = 0; i < 2; i++) {
       bf16x8 k[KS];
@@ -227,7 +226,7 @@ __device__ __forceinline__ void few_rows4(const AttnCtx& c, const unsigned id) {
     unsigned n[NB];
 #pragma unroll
     for (int nb = 0; nb < NB; nb++) { lo[nb] = (beam_q[nb] - beam0) * c.u - oj * FT; n[nb] = qrow[nb] >= 0 ? (unsigned)c.u : 0u; }
-    softmax_pv(s, lo, n, false, [] {});
+    softmax_pv(s, lo, n, false);
   }
   };
 
@@ -259,20 +258,20 @@ __device__ __forceinline__ void few_rows4(const AttnCtx& c, const unsigned id) {
       locate(j + WAVES);
       k = load(k_head, k_off, kp_off);
     }
+#pragma unroll
+    for (int i = 0; i < 2; i++) {
+      // (rows behind the list hold anything, and must not be infinite times 0)
+      const uint32_t power = all || 16 * i + vr < left ? v.power[i] : 127u;
+#pragma unroll
+      for (int w = 0; w < NW; w++) put_v(i, w, __builtin_bit_cast(u32x4, fp4_values8(v.w[i][w], power)));
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (more) v = load(v_head, v_off, vp_off);
     int lo[NB];
     unsigned n[NB];
 #pragma unroll
     for (int nb = 0; nb < NB; nb++) { lo[nb] = 0; n[nb] = (unsigned)left; }
-    softmax_pv(s, lo, n, all, [&] {
-#pragma unroll
-      for (int i = 0; i < 2; i++) {
-        // (rows behind the list hold anything, and must not be infinite times 0)
-        const uint32_t power = all || 16 * i + vr < left ? v.power[i] : 127u;
-#pragma unroll
-        for (int w = 0; w < NW; w++) put_v(i, w, __builtin_bit_cast(u32x4, fp4_values8(v.w[i][w], power)));
-      }
-      if (more) v = load(v_head, v_off, vp_off);
-    });
+    softmax_pv(s, lo, n, all);
   }
 
   // ---- the wavefronts' parts join in LDS, 16 rows at a time; then every one has columns of its own to write
