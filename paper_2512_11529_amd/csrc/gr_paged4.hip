@@ -14,7 +14,10 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 // 16 * NB rows of a (request, KV head) pair against a segment of its keys.  The wavefronts hold the same rows and take 32 tokens each in turn; nobody waits for
 // anybody until their (maximum, sum, O) are joined in LDS.
-// Bound: memory (17/32 byte an element).
+// Bound: memory (17/32 byte an element).  us: 64 requests of 14208 tokens x 1 beam, 32 and 8 heads of 128, 172 (5.75 TB/s; a plain read of 1 GiB reaches 6.3), 32 of 12001-16384 x 2, whose 256
+// workgroups end with the longest list, 95 (5.1); the same loads without anything done to what they bring 87.  Vector instructions (160 for a tile of one block) keep the SIMDs busy 37 % of that time.
+// Tried: two tiles on their way instead of one 96-104; 128 registers for four wavefronts to a SIMD, with spills, 100-159; V asked for ahead of K 102; the powers of K and V in one load,
+// spread by ds_bpermute, 95 (and 3 % more where the loads are not waited for); 48 rows a wavefront, for many rows, 482 against 495 with 32 and 329 with gr_beam_attn's body.
 template <int D>
 struct Fp4 {
   static constexpr int FT = 32;                    // tokens of a tile: two halves of 16
@@ -336,7 +339,8 @@ __global__ void __launch_bounds__(WAVES * 64) __attribute__((amdgpu_waves_per_eu
   few_rows4<D, NB, WAVES, 0>(c, blockIdx.x);
 }
 
-// Blocks of 128 and 256 rows: gr_beam_attn's body.
+// Blocks of 128 and 256 rows: gr_beam_attn's body, bound as it is by the issue rate of matrix instructions, softmax and LDS reads: 32 requests of 512-3700 tokens x 256 beams behind 256, 32 and 8
+// heads of 128, 329 us (1.0 PFLOP/s; bf16 pages 313-324).  By blocks of 32 rows whose wavefronts share out the keys 495.
 template <int D, int NWAVES, int KS, bool FIND>
 __global__ void __launch_bounds__(NWAVES * 64 * KS) __attribute__((amdgpu_waves_per_eu(2, 2))) k_fp4_attn(AttnCtx c) {
   constexpr int NCB = 1;
@@ -345,7 +349,8 @@ __global__ void __launch_bounds__(NWAVES * 64 * KS) __attribute__((amdgpu_waves_
 }
 
 
-// A packed prefix by blocks of 128 rows of all requests, which are dealt first (arguments c), and each request's list by blocks of 16 or 32 (arguments few).
+// A packed prefix by blocks of 128 rows of all requests, which are dealt first (arguments c), and each request's list by blocks of 16 or 32 (arguments few).  64 requests of 16-600 tokens x 4
+// beams behind 4096 common ones 31 us, and 6 for the join, 34 among others (in blocks of 16 rows over the whole lists 46): 16 tiles a workgroup, one to a CU.
 constexpr int fp4_mix_lds_bytes(int d, int nb) { return attn_lds_bytes(d, 128, 1) > fp4_few_lds_bytes(d, nb, 4) ? attn_lds_bytes(d, 128, 1) : fp4_few_lds_bytes(d, nb, 4); }
 template <int D, int NB>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) k_fp4_mix(AttnCtx c, AttnCtx few, unsigned blocks0) {

@@ -7,6 +7,8 @@
 // Bound: memory, 4 bytes an element in and out (bf16).  A lane holds 16 elements of a head in two runs of eight, so that both of every pair are its own: elements 8 j .. and
 // rot / 2 + 8 j .., or 16 j .. .  4, 8 or 16 lanes hold the head, and a wavefront the same head of 16, 8 or 4 consecutive rows: what it writes into an FP4 page is then one
 // run of codes and one of scales, and a lane's cosines and sines serve all of its heads.  The wavefronts of a workgroup take different heads of the same rows.
+// With 16 consecutive elements a lane and the other halves of its pairs loaded a second time, 32 x 256 rows of 32 + 8 + 8 heads of 128, normed, took 69.6 us, now 40.9 (4.9 TB/s; a copy of
+// 1 GiB reaches 5.15), 32 x 4096 tokens of 8 heads into FP4 361 us, now 146 (4.7).  The launch is all there is of 16 rows of 8 + 8 + 8 heads of 64: 2.7 us.
 #include <initializer_list>
 #include <type_traits>
 #include "gr_pages.hpp"
@@ -229,14 +231,18 @@ __global__ void __launch_bounds__(256) k_page_append(AppendCtx c) {
   const uint32_t slot = (uint32_t)c.slot[at.row];
   const bool stores = at.live && at.holds && slot < c.n_slots;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), h0 = ((int)at.chunk * 4 + wave) * U, heads = 2 * c.Hkv;
+  const int64_t k_row = (int64_t)at.row * c.k_stride, v_row = (int64_t)at.row * c.v_stride;
   Head x[U];
 #pragma unroll
   for (int u = 0; u < U; u++) {
     const int h = min(h0 + u, heads - 1);
-    x[u].load(h < c.Hkv ? c.k + (int64_t)at.row * c.k_stride + h * c.t.d : c.v + (int64_t)at.row * c.v_stride + (h - c.Hkv) * c.t.d, at);
+    x[u].load(h < c.Hkv ? c.k + h * c.t.d + k_row : c.v + (h - c.Hkv) * c.t.d + v_row, at);
   }
   const Angles a(c.t, at, PAIRS);
   Weights ws;
+  // FP4: bytes from a pool's first record of a head to the row's codes, and from these to its powers
+  const uint32_t ps = 1u << c.shift, d = (uint32_t)c.t.d, tok = slot & (ps - 1), record = gr_fp4_record(ps, d), powers_at = gr_fp4_codes(ps, d) + tok * (d / 32) - tok * (d / 2);
+  const size_t codes_at = (size_t)(slot >> c.shift) * ((unsigned)c.Hkv * record) + tok * (d / 2);
   // largest of each eight of the wavefront's heads: a block's are four neighbours there, wherever its lanes are
   __shared__ __attribute__((aligned(16))) uint32_t s_most[KV == GR_KV_FP4 ? 4 * 128 : 4];
 #pragma unroll
@@ -250,33 +256,32 @@ __global__ void __launch_bounds__(256) k_page_append(AppendCtx c) {
     else x[u].numbers(y);
     uint8_t* pages = is_k ? c.k_pages : c.v_pages;
     if (KV == GR_KV_FP4) {
-      const uint32_t ps = 1u << c.shift, tok = slot & (ps - 1), d = (uint32_t)c.t.d;
       uint32_t* most = s_most + wave * 128 + ((int)threadIdx.x & 63) / LG * (2 * LG);
       if (at.holds) {
 #pragma unroll
         for (int r = 0; r < 2; r++) {
-          uint32_t m = 0;
+          float m = 0.f;
 #pragma unroll
-          for (int e = 0; e < 8; e++) m = max(m, __float_as_uint(y[8 * r + e]) & 0x7fffffffu);       // (as whole numbers: NaN is above the infinite)
-          most[at.e[r] >> 3] = m;
+          for (int e = 0; e < 8; e++) m = __builtin_elementwise_maximum(m, __builtin_fabsf(y[8 * r + e]));        // (NaN stays)
+          most[at.e[r] >> 3] = __float_as_uint(m) & 0x7fffffffu;
         }
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");             // (the wavefront's own places, and LDS serves it in order)
-      uint8_t* record = pages + ((size_t)(slot >> c.shift) * (unsigned)c.Hkv + (unsigned)h) * gr_fp4_record(ps, d);
+      uint8_t* codes = pages + (unsigned)h * record + codes_at;
 #pragma unroll
       for (int r = 0; r < 2; r++) {
         const uint32_t e = (uint32_t)at.e[r];
         const uint4 m4 = *(const uint4*)(most + (e >> 5) * 4);
-        const uint32_t m = max(max(m4.x, m4.y), max(m4.z, m4.w)), power = fp4_power(m);
+        const uint32_t m = max(max(m4.x, m4.y), max(m4.z, m4.w)), power = fp4_power(m);                 // (as whole numbers: NaN is above the infinite)
         if (stores) {
-          *(uint32_t*)(record + tok * (d / 2) + e / 2) = fp4_codes8(y + 8 * r, power);
+          *(uint32_t*)(codes + e / 2) = fp4_codes8(y + 8 * r, power);
           // (an infinite value or NaN makes the scale one that says NaN for all 32)
-          if ((e & 31) == 0) record[gr_fp4_codes(ps, d) + tok * (d / 32) + e / 32] = (uint8_t)(m >= 0x7f800000u ? 255u : power);
+          if ((e & 31) == 0) codes[powers_at + e / 32] = (uint8_t)(m >= 0x7f800000u ? 255u : power);
         }
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     } else {
-      const size_t i = ((size_t)slot * (unsigned)c.Hkv + (unsigned)h) * (unsigned)c.t.d;
+      const size_t i = (size_t)slot * ((unsigned)c.Hkv * d) + (unsigned)h * d;
       if (KV == GR_KV_BF16) {
         if (stores) store16((uint16_t*)pages + i, at, y);
       } else {
