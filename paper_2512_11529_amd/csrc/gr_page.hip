@@ -212,8 +212,9 @@ struct ReadCtx {
 };
 
 // Bound: memory, 4 bytes an element in and out (FP8 3, FP4 2.5).  A lane takes 16 consecutive elements of a head, a wavefront the same head of 64 / LG consecutive rows: of
-// FP4 pages, whose tokens of a head lie together, it reads runs of codes and of scales.  One head a wavefront: 32 x 4096 tokens of 8 heads of 128 out of FP4 130 us (5.2 TB/s; a copy of 1 GiB
-// reaches 5.15), 32 prompts of 512-3700 tokens 80 us (4.6).
+// FP4 pages, whose tokens of a head lie together, it reads runs of codes and of scales.  Two heads a wavefront: 32 x 4096 tokens of 8 heads of 128 out of FP4 124 us (5.5 TB/s; a copy
+// of 1 GiB reaches 5.15), 32 prompts of 512-3700 tokens 78 us (4.7); one 130 and 79, four 159 and 95.
+constexpr int kReadHeads = 2;
 template <int LG, int KV>
 __global__ void __launch_bounds__(256) k_page_read(ReadCtx c) {
   uint32_t group = __umulhi(blockIdx.x, c.inv_chunks);
@@ -224,39 +225,50 @@ __global__ void __launch_bounds__(256) k_page_read(ReadCtx c) {
   if (row >= c.T || e0 >= d) return;
   const uint32_t slot = (uint32_t)c.slot[row];
   if (slot >= c.n_slots) return;
-  const int h = (int)chunk * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-  if (h >= heads) return;
-  const bool is_k = h < c.Hkv;
-  const unsigned hk = (unsigned)(is_k ? h : h - c.Hkv);
-  const uint8_t* pages = is_k ? c.k_pages : c.v_pages;
-  kv_u32x4 y[2];
-  if (KV == GR_KV_FP4) {
-    const uint32_t ps = 1u << c.shift, tok = slot & (ps - 1);
-    const uint8_t* record = pages + ((size_t)(slot >> c.shift) * (unsigned)c.Hkv + hk) * gr_fp4_record(ps, d);
-    const kv_u32x2 w = *(const kv_u32x2*)(record + tok * (d / 2) + e0 / 2);
-    const uint32_t power = record[gr_fp4_codes(ps, d) + tok * (d / 32) + e0 / 32];
+  const int h0 = ((int)chunk * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6)) * kReadHeads;
+  kv_u32x4 y[kReadHeads][2];
+  uint32_t power[kReadHeads];
 #pragma unroll
-    for (int p = 0; p < 2; p++) y[p] = power == 255u ? kv_u32x4{0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u} : fp4_values8(w[p], power);      // (255: no numbers)
-  } else {
-    const size_t i = ((size_t)slot * (unsigned)c.Hkv + hk) * d + e0;
-    if (KV == GR_KV_FP8) {
-      const kv_u32x4 w = *(const kv_u32x4*)(pages + i);
+  for (int u = 0; u < kReadHeads; u++) {
+    const int h = min(h0 + u, heads - 1);
+    const bool is_k = h < c.Hkv;
+    const unsigned hk = (unsigned)(is_k ? h : h - c.Hkv);
+    const uint8_t* pages = is_k ? c.k_pages : c.v_pages;
+    if (KV == GR_KV_FP4) {
+      const uint32_t ps = 1u << c.shift, tok = slot & (ps - 1);
+      const uint8_t* record = pages + ((size_t)(slot >> c.shift) * (unsigned)c.Hkv + hk) * gr_fp4_record(ps, d);
+      const kv_u32x2 w = *(const kv_u32x2*)(record + tok * (d / 2) + e0 / 2);
+      y[u][0] = kv_u32x4{w[0], w[1], 0, 0};
+      power[u] = record[gr_fp4_codes(ps, d) + tok * (d / 32) + e0 / 32];
+    } else {
+      const uint8_t* from = pages + (((size_t)slot * (unsigned)c.Hkv + hk) * d + e0) * (KV == GR_KV_FP8 ? 1 : 2);
+      y[u][0] = *(const kv_u32x4*)from;
+      if (KV == GR_KV_BF16) y[u][1] = *(const kv_u32x4*)(from + 16);
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < kReadHeads; u++) {
+    const int h = h0 + u;
+    if (h >= heads) return;
+    const bool is_k = h < c.Hkv;
+    if (KV == GR_KV_FP4) {
+      const uint32_t w[2] = {y[u][0][0], y[u][0][1]};
+#pragma unroll
+      for (int p = 0; p < 2; p++) y[u][p] = power[u] == 255u ? kv_u32x4{0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u} : fp4_values8(w[p], power[u]);      // (255: no numbers)
+    } else if (KV == GR_KV_FP8) {
+      const kv_u32x4 w = y[u][0];
       const float scale = is_k ? c.k_scale : c.v_scale;
 #pragma unroll
       for (int k = 0; k < 4; k++) {
         const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[k], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[k], true);
-        y[k / 2][2 * (k % 2)] = bf16_pair(lo[0] * scale, lo[1] * scale);
-        y[k / 2][2 * (k % 2) + 1] = bf16_pair(hi[0] * scale, hi[1] * scale);
+        y[u][k / 2][2 * (k % 2)] = bf16_pair(lo[0] * scale, lo[1] * scale);
+        y[u][k / 2][2 * (k % 2) + 1] = bf16_pair(hi[0] * scale, hi[1] * scale);
       }
-    } else {
-      const kv_u32x4* from = (const kv_u32x4*)((const uint16_t*)pages + i);
-      y[0] = from[0];
-      y[1] = from[1];
     }
+    kv_u32x4* to = (kv_u32x4*)(is_k ? c.k + (int64_t)row * c.k_stride + h * c.d + e0 : c.v + (int64_t)row * c.v_stride + (h - c.Hkv) * c.d + e0);
+    to[0] = y[u][0];
+    to[1] = y[u][1];
   }
-  kv_u32x4* to = (kv_u32x4*)(is_k ? c.k + (int64_t)row * c.k_stride + hk * d + e0 : c.v + (int64_t)row * c.v_stride + hk * d + e0);
-  to[0] = y[0];
-  to[1] = y[1];
 }
 
 }  // namespace
@@ -344,7 +356,7 @@ extern "C" gr_status gr_page_read(const gr_page_read_params* p, void* stream_) {
   c.k_pages = (const uint8_t*)p->k_pages; c.v_pages = (const uint8_t*)p->v_pages; c.slot = p->slot; c.k = (uint16_t*)p->k; c.v = (uint16_t*)p->v;
   auto go = [&](auto lanes, auto type) {
     constexpr int LG = decltype(lanes)::value, KV = decltype(type)::value;
-    c.chunks = (uint32_t)((2 * p->Hkv + 3) / 4);
+    c.chunks = (uint32_t)((2 * p->Hkv + 4 * kReadHeads - 1) / (4 * kReadHeads));
     c.inv_chunks = 0xffffffffu / c.chunks;
     const int64_t grid = (p->T + 64 / LG - 1) / (64 / LG) * c.chunks;
     if (!gr_grid_fits(grid, 256)) return (gr_status)GR_ERR_UNSUPPORTED;
