@@ -113,11 +113,16 @@ __device__ __forceinline__ int request_by_own_length(const AttnCtx& c, int rank,
   for (int k = 0; k < 2; k++) l[k] = lane + 64 * k < c.B ? paged_length(c, lane + 64 * k) : -1;
   return request_of_rank(first, l, rank, lane, &none, len);
 }
-// Number of page p of a request's list (behind the last one: that one's); one outside the pool counts as 0.
+// Number of page p of a request's list (behind the last one: that one's), as its table has it; one outside the pool counts as 0.
+template <class C>
+__device__ __forceinline__ int page_entry(const C& c, unsigned b, int p, int last) {
+  p = min(p, last);
+  const int q = p - (c.front >> c.shift);
+  return q < 0 ? c.prefix_pages[p] : c.table[(size_t)b * (unsigned)c.max_pages + (unsigned)q];
+}
 template <class C>
 __device__ __forceinline__ int page_number(const C& c, unsigned b, int p, int last) {
-  p = min(p, last);
-  const int q = p - (c.front >> c.shift), number = q < 0 ? c.prefix_pages[p] : c.table[(size_t)b * (unsigned)c.max_pages + (unsigned)q];
+  const int number = page_entry(c, b, p, last);
   return (unsigned)number < (unsigned)c.n_pages ? number : 0;
 }
 // Slot of token t of the list in the pools.

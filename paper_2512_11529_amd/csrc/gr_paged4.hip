@@ -14,9 +14,9 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 // 16 * NB rows of a (request, KV head) pair against a segment of its keys.  The wavefronts hold the same rows and take 32 tokens each in turn; nobody waits for
 // anybody until their (maximum, sum, O) are joined in LDS.
-// Bound: memory (17/32 byte an element).  us: 64 requests of 14208 tokens x 1 beam, 32 and 8 heads of 128, 172 (5.75 TB/s; a plain read of 1 GiB reaches 6.3), 32 of 12001-16384 x 2, whose 256
-// workgroups end with the longest list, 95 (5.1); the same loads without anything done to what they bring 87.  Vector instructions (160 for a tile of one block) keep the SIMDs busy 37 % of that time.
-// Tried: two tiles on their way instead of one 96-104; 128 registers for four wavefronts to a SIMD, with spills, 100-159; V asked for ahead of K 102; the powers of K and V in one load,
+// Bound: memory (17/32 byte an element).  us: 64 requests of 14208 tokens x 1 beam, 32 and 8 heads of 128, 170 (5.8 TB/s; a plain read of 1 GiB reaches 6.3), 32 of 12001-16384 x 2, whose 256
+// workgroups end with the longest list, 94 (5.2); the same loads without anything done to what they bring 87.  Vector instructions (160 for a tile of one block) keep the SIMDs busy 37 % of that time.
+// Tried: the operands of V kept in order behind scheduling barriers 96.4 instead of 93.9; two tiles on their way instead of one 96-104; 128 registers for four wavefronts to a SIMD, with spills, 100-159; V asked for ahead of K 102; the powers of K and V in one load,
 // spread by ds_bpermute, 95 (and 3 % more where the loads are not waited for); 48 rows a wavefront, for many rows, 482 against 495 with 32 and 329 with gr_beam_attn's body.
 template <int D>
 struct Fp4 {
@@ -48,8 +48,9 @@ __device__ __forceinline__ void few_rows4(const AttnCtx& c, const unsigned id) {
 
   // ---- page numbers: lane i has that of page window + i of the list, and `ahead` that of the 64th after it
   const int most_pages = (c.front + c.max_L + (1 << c.shift) - 1) >> c.shift;
-  auto numbers_from = [&](int first) { return most_pages > 0 ? page_number(c, bu, first + lane, most_pages - 1) : 0; };
-  int window = 0, numbers = sp == 0 ? numbers_from(0) : 0;
+  auto entries_from = [&](int first) { return most_pages > 0 ? page_entry(c, bu, first + lane, most_pages - 1) : 0; };
+  auto checked = [&](int entry) { return (unsigned)entry < (unsigned)c.n_pages ? entry : 0; };
+  int window = 0, numbers = sp == 0 ? entries_from(0) : 0;   // (checked when they are needed: the loads are waited for there)
   const int keys = c.front + __builtin_amdgcn_readfirstlane(paged_length(c, (int)bu));
 
   // ---- Q: lane (row n16, quarter h) has the elements of K's quarter, in K's order
@@ -72,8 +73,9 @@ __device__ __forceinline__ void few_rows4(const AttnCtx& c, const unsigned id) {
   const bool own_stage = c.u > 0 && sp == (max(0, keys - (ns - 1) * chunk) < chunk ? ns - 1 : 0);
   const int Ru = own_stage ? (__builtin_amdgcn_readfirstlane(small_div(min(row_w + ROWS - 1, M - 1), c.rcp_g)) - beam0 + 1) * c.u : 0;
   const int n_own = (Ru + FT - 1) / FT;
-  if (sp > 0) { window = seg0 >> c.shift; numbers = numbers_from(window); }
-  int ahead = numbers_from(window + 64);
+  if (sp > 0) { window = seg0 >> c.shift; numbers = entries_from(window); }
+  int ahead = entries_from(window + 64);
+  numbers = checked(numbers);
 
   // ---- a tile's codes and powers in registers: halves of 16 tokens, each of which lies in one page
   struct Codes { typename F::words w[2]; uint32_t power[2]; };
@@ -92,8 +94,8 @@ __device__ __forceinline__ void few_rows4(const AttnCtx& c, const unsigned id) {
       const int tok = seg0 + j * FT + 16 * i, p = tok >> c.shift;
       if (p - window >= 64) {                                // (wave-uniform; both halves of a tile are in one window)
         window += 64;
-        numbers = ahead;
-        ahead = numbers_from(window + 64);
+        numbers = checked(ahead);
+        ahead = entries_from(window + 64);
       }
       page_at[i] = (size_t)(unsigned)__builtin_amdgcn_readlane(numbers, p - window) * page_bytes;
       in_at[i] = (uint32_t)tok & (ps - 1);
@@ -131,17 +133,27 @@ __device__ __forceinline__ void few_rows4(const AttnCtx& c, const unsigned id) {
   typedef s16x4 __attribute__((address_space(3))) * lds_s16x4;
   auto put_v = [&](int i, int piece, u32x4 x) { *(lds_u32x4)(uintptr_t)(uint32_t)(w_at[piece / 2] + 16 * D * 2 * i + 16 * (piece & 1)) = x; };
 
-  // The tile's scores to probabilities and onto O; V is in LDS.  rows [lo, lo + n) of the tile are seen by the column.
-  auto softmax_pv = [&](f32x4 (&s)[2][NB], const int (&lo)[NB], const unsigned (&n)[NB], bool all) __attribute__((always_inline)) {
-    bf16x8 p[NB];
+  auto read_v = [&](int db) {
+    typedef short s16x8 __attribute__((ext_vector_type(8)));
+    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)(uint32_t)(r_at ^ (32 * db)));
+    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)(uint32_t)((r_at ^ (32 * db)) + 16 * D * 2));
+    return __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+  };
+  // rows [lo, lo + n) of the tile are seen by column nb
+  auto mask = [&](f32x4 (&s)[2][NB], int nb, int lo, unsigned n) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 2; i++)
+#pragma unroll
+      for (int e = 0; e < 4; e++) s[i][nb][e] = (unsigned)(16 * i + 4 * h + e - lo) < n ? s[i][nb][e] : -INFINITY;
+  };
+  // The tile's scores to probabilities and onto O; V is in LDS, whose first operands are on their way meanwhile and the others PF matrix instructions' time.
+  auto softmax_pv = [&](f32x4 (&s)[2][NB]) __attribute__((always_inline)) {
+    constexpr int PF = NB == 1 ? 2 : 3;                      // (read where they are needed: 8 requests of 2000-4000 x 8 beams 18.2 us, 16.9; 16 of 3000 x 16 25.9, 24.4)
+    bf16x8 p[NB], v[DB];
+#pragma unroll
+    for (int db = 0; db < PF; db++) v[db] = read_v(db);
 #pragma unroll
     for (int nb = 0; nb < NB; nb++) {
-      if (!all) {
-#pragma unroll
-        for (int i = 0; i < 2; i++)
-#pragma unroll
-          for (int e = 0; e < 4; e++) s[i][nb][e] = (unsigned)(16 * i + 4 * h + e - lo[nb]) < n[nb] ? s[i][nb][e] : -INFINITY;
-      }
       float mx = -INFINITY;
 #pragma unroll
       for (int i = 0; i < 2; i++)
@@ -149,7 +161,7 @@ __device__ __forceinline__ void few_rows4(const AttnCtx& c, const unsigned id) {
         for (int e = 0; e < 4; e++) mx = fmaxf(mx, s[i][nb][e]);
       mx *= c.c;
       // (a column's reference rises when a score is more than 8 above it: probabilities of up to 2^8, as in gr_beam_attn)
-      if (__any(mx > m_run[nb] + AttnTile<D, 1>::kLazy)) {
+      if (__builtin_expect(__any(mx > m_run[nb] + AttnTile<D, 1>::kLazy), 0)) {
         float top = fmaxf(mx, __shfl_xor(mx, 16, 64));
         top = fmaxf(top, __shfl_xor(top, 32, 64));
         const float m_new = top > m_run[nb] ? top : m_run[nb];
@@ -161,6 +173,9 @@ __device__ __forceinline__ void few_rows4(const AttnCtx& c, const unsigned id) {
 #pragma unroll
           for (int e = 0; e < 4; e++) o[db][nb][e] *= scale;
       }
+    }
+#pragma unroll
+    for (int nb = 0; nb < NB; nb++) {
       const float ref = m_run[nb] > -INFINITY ? m_run[nb] : 0.f;
 #pragma unroll
       for (int i = 0; i < 2; i++)
@@ -173,12 +188,9 @@ __device__ __forceinline__ void few_rows4(const AttnCtx& c, const unsigned id) {
     }
 #pragma unroll
     for (int db = 0; db < DB; db++) {
-      typedef short s16x8 __attribute__((ext_vector_type(8)));
-      const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)(uint32_t)(r_at ^ (32 * db)));
-      const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)(uint32_t)((r_at ^ (32 * db)) + 16 * D * 2));
-      const bf16x8 v = __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+      if (db + PF < DB) v[db + PF] = read_v(db + PF);
 #pragma unroll
-      for (int nb = 0; nb < NB; nb++) o[db][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[nb], o[db][nb], 0, 0, 0);
+      for (int nb = 0; nb < NB; nb++) o[db][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[db], p[nb], o[db][nb], 0, 0, 0);
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // (LDS serves a wavefront in order: the next tile's V goes where this one's was)
   };
@@ -225,11 +237,9 @@ __device__ __forceinline__ void few_rows4(const AttnCtx& c, const unsigned id) {
         for (int st = 0; st < KS; st++) s[i][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[st], q[nb][st], s[i][nb], 0, 0, 0);
       }
     }
-    int lo[NB];
-    unsigned n[NB];
 #pragma unroll
-    for (int nb = 0; nb < NB; nb++) { lo[nb] = (beam_q[nb] - beam0) * c.u - oj * FT; n[nb] = qrow[nb] >= 0 ? (unsigned)c.u : 0u; }
-    softmax_pv(s, lo, n, false);
+    for (int nb = 0; nb < NB; nb++) mask(s, nb, (beam_q[nb] - beam0) * c.u - oj * FT, qrow[nb] >= 0 ? (unsigned)c.u : 0u);
+    softmax_pv(s);
   }
   };
 
@@ -242,9 +252,9 @@ __device__ __forceinline__ void few_rows4(const AttnCtx& c, const unsigned id) {
     v = load(v_head, v_off, vp_off);
   }
   own_tokens();
-  for (; j < nt; j += WAVES) {
-    const int left = seg1 - (seg0 + j * FT);
-    const bool all = left >= FT, more = j + WAVES < nt;
+  auto tile = [&](auto last) __attribute__((always_inline)) {
+    constexpr bool LAST = decltype(last)::value;             // of this wavefront: the only one that may be partial, and none is asked for
+    const int left = LAST ? seg1 - (seg0 + j * FT) : FT;
     f32x4 s[2][NB];
 #pragma unroll
     for (int i = 0; i < 2; i++) {
@@ -257,24 +267,28 @@ __device__ __forceinline__ void few_rows4(const AttnCtx& c, const unsigned id) {
         for (int nb = 0; nb < NB; nb++) s[i][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, q[nb][st], s[i][nb], 0, 0, 0);
       }
     }
-    if (more) {
+    if (!LAST) {
       locate(j + WAVES);
       k = load(k_head, k_off, kp_off);
     }
 #pragma unroll
     for (int i = 0; i < 2; i++) {
       // (rows behind the list hold anything, and must not be infinite times 0)
-      const uint32_t power = all || 16 * i + vr < left ? v.power[i] : 127u;
+      const uint32_t power = !LAST || 16 * i + vr < left ? v.power[i] : 127u;
 #pragma unroll
       for (int w = 0; w < NW; w++) put_v(i, w, __builtin_bit_cast(u32x4, fp4_values8(v.w[i][w], power)));
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    if (more) v = load(v_head, v_off, vp_off);
-    int lo[NB];
-    unsigned n[NB];
+    if (!LAST) v = load(v_head, v_off, vp_off);
+    if (LAST && left < FT) {
 #pragma unroll
-    for (int nb = 0; nb < NB; nb++) { lo[nb] = 0; n[nb] = (unsigned)left; }
-    softmax_pv(s, lo, n, all);
+      for (int nb = 0; nb < NB; nb++) mask(s, nb, 0, (unsigned)left);
+    }
+    softmax_pv(s);
+  };
+  if (j < nt) {
+    for (; j + WAVES < nt; j += WAVES) tile(std::false_type());
+    tile(std::true_type());
   }
 
   // ---- the wavefronts' parts join in LDS, 16 rows at a time; then every one has columns of its own to write
