@@ -96,23 +96,30 @@ constexpr PagedCost kPagedCost[2][2] = {      // [head size 128][FP8]; rate in b
     {{3.3, 1.5, 1.2, 2.0, 2.0, 1.05, 0.95, 1.5, 0.7, 3.1, 8.0e6}, {3.3, 1.5, 1.4, 2.0, 2.0, 1.05, 0.95, 1.5, 0.8, 3.1, 4.0e6}},
     {{0.7, 0.15, 1.9, 1.95, 2.1, 0.9, 1.25, 0.4, 0.9, 1.95, 7.9e6}, {1.5, 2.35, 2.05, 1.6, 4.0, 1.45, 1.35, 1.25, 0.9, 2.2, 5.4e6}}};
 
-// FP4, up to 80 rows of a pair: the same choice by estimated time, over blocks of 16 rows (32 for more than 16) with four or, ks = 2, eight wavefronts, blocks of 128 for more than 24, and the
-// prefix packed.  few16 and few32 are a block's fixed time and their steps those of 128 tokens for four wavefronts (`eight` more, and half the steps, for eight), per_cu such
-// blocks of four wavefronts share a CU.  Fitted to 9170 random calls of 1 to 128 requests of 10 to 16384 tokens with 1 to 80 rows, half of them behind a prefix of 64 to 8192 tokens, each timed in up to 50 ways:
-// with them the mean call takes 1.026 times the best of its ways, one in twenty more than 1.15 (1.05 and 1.25 without a join's time for each segment: 32 of them for 2000 tokens), the worst 1.6: a few rows of ragged or very long lists left in one segment.
-struct Fp4Cost { double start, few16, step16, per_cu16, few32, step32, per_cu32, eight, unit, tile1, tile2, shared, shared_tile, join, join_one, rate; };      // join_one: for each segment
-constexpr Fp4Cost kFp4Cost[2] = {{3.84, 1.55, 0.63, 2.66, 1.76, 0.74, 1.56, 0.39, 1.54, 1.03, 0.99, 1.15, 0.75, 1.5, 0.25, 5.9e6},
-                                 {4.85, 1.63, 0.74, 1.68, 2.47, 1.01, 1.53, 0.51, 2.17, 1.47, 1.36, 0.83, 1.13, 1.5, 0.1, 4.7e6}};
+// FP4: the same choice by estimated time, for any number of rows: blocks of 16 rows (32 for more than 16) with four or, ks = 2, eight wavefronts for up to 160 rows of a pair, of 128 (ks = 2 with
+// two sets of wavefronts where there is at most one to a CU) for more than 24, of 256 for more than 128, each with 1 to 16 (32) segments, and up to 80 rows the prefix packed.  A block's time is a
+// fixed part and a step for its tokens, 128 of them (few16, few32; `eight` more, and half the steps, with eight wavefronts) or 64 (rows128, two sets, rows256), times the rounds that an XCD's 32 CUs
+// take the blocks in, between their number (weight 1 - ceil) and the whole one above (weight ceil), with per_cu16, per_cu32, 2, 1 and 1 blocks to a CU; the fourth root of the sum of its fourth power and
+// that of the keys' time at `rate`; and for several segments `join`, `join_one` for each, and partials at `partials` bytes a us.
+// Fitted to half of 13450 random calls of 1 to 128 requests of 10 to 16384 tokens with 1 to 2048 rows, half of them behind a prefix of 64 to 8192 tokens, each timed in up to 50 ways: of the other half
+// the mean call takes 1.019 times the best of its ways, one in twenty more than 1.11, the worst 1.6 (a few ragged or very long lists left in one segment).  With gr_beam_attn's rule for FP8 the calls
+// of more than 80 rows took 1.043 times their best (16 x 4000 tokens x 200 beams 240 us in blocks of 128 rows, which widen every key more often, 229 in blocks of 256).
+struct Fp4Cost {
+  double start, few16, step16, per_cu16, few32, step32, per_cu32, eight, ceil_few, rows128, tile128, sets, tile_sets, rows256, tile256, ceil_rows, shared, shared_tile, join, join_one, partials, rate;
+};
+constexpr Fp4Cost kFp4Cost[2] = {{4.23, 1.70, 0.562, 3.67, 2.36, 0.725, 1.88, 0.38, 0.30, 2.96, 1.05, 1.97, 1.12, 3.08, 1.05, 0.45, 1.09, 0.66, 1.44, 0.26, 4.0e6, 4.8e6},
+                                 {6.02, 1.42, 0.763, 1.88, 2.36, 1.115, 1.76, 0.56, 0.18, 1.82, 1.49, 2.38, 1.58, 4.10, 1.25, 0.67, 0.76, 1.27, 1.20, 0.21, 3.8e6, 6.75e6}};
 PagedPlan plan_fp4(const gr_attn_paged_params* p) {
   PagedPlan plan{};
   const int64_t M = (int64_t)p->W * (p->Hq / p->Hkv), all = p->B * M, pairs = (int64_t)p->B * p->Hkv, list = (int64_t)p->prefix_L + p->max_L;
   const Fp4Cost& c = kFp4Cost[p->d == 128];
   const int rows = M <= 16 ? 16 : 32;
   const double few0 = rows == 16 ? c.few16 : c.few32, step = rows == 16 ? c.step16 : c.step32, per_cu = rows == 16 ? c.per_cu16 : c.per_cu32;
-  const double partial_us = 2.0 * p->B * p->W * p->Hq * p->d * 4 / 2.7e6, token_bytes = 17.0 / 16 * p->Hkv * p->d;
+  const double partial_us = 2.0 * p->B * p->W * p->Hq * p->d * 4 / c.partials, token_bytes = 17.0 / 16 * p->Hkv * p->d;
   auto parts = [](int64_t n, int64_t of) { return (n + of - 1) / of; };
   auto larger = [](double a, double b) { return a > b ? a : b; };
   auto both = [](double a, double b) { return sqrt(sqrt(a * a * a * a + b * b * b * b)); };
+  auto rounds = [&](double blocks, double places, double weight) { return larger(1.0, weight * ceil(blocks / places) + (1.0 - weight) * (blocks / places)); };
   double least = 0;
   auto look_at = [&](int r, int n0, int n1, int ks, double us) {
     const int n = n0 + n1;
@@ -124,19 +131,25 @@ PagedPlan plan_fp4(const gr_attn_paged_params* p) {
   const double list_us = list * p->B * token_bytes / c.rate;
   for (const int n : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
     if (n > 1 && n * 64 > list) break;
-    const double tiles = (double)parts(parts(list, n), KT), blocks = (double)(parts(pairs * n, 8) * parts(M, rows));
-    for (const int ks : {1, 2}) {
-      const double few = few0 + step * tiles / (2 * ks) + (ks == 2 ? c.eight : 0.0);
-      look_at(rows, 0, n, ks, both(few * larger(1.0, blocks * ks / (32 * per_cu)), list_us));
-    }
-    if (M <= 24 || n > 16) continue;
+    const double tiles = (double)parts(parts(list, n), KT);
     const int64_t on_xcd = parts(pairs * n, 8);
-    const bool sets = list > KT && pairs * n <= 256;
-    const double unit = sets ? (c.unit + c.tile2 * (double)(((int64_t)tiles + 1) >> 1)) * (double)parts(on_xcd, 32) : (c.unit + c.tile1 * tiles) * larger(1.0, on_xcd / 64.0);
-    look_at(128, 0, n, sets ? 2 : 1, both(unit, list_us));
+    if (M <= 160) {
+      for (const int ks : {1, 2}) {
+        const double few = few0 + step * tiles / (2 * ks) + (ks == 2 ? c.eight : 0.0);
+        look_at(rows, 0, n, ks, both(few * rounds((double)(on_xcd * parts(M, rows) * ks), 32 * per_cu, c.ceil_few), list_us));
+      }
+    }
+    if (M <= 24 || n > 16 || (n > 1 && n * 96 > list)) continue;
+    for (const int r : {128, 256}) {
+      const int64_t units = pairs * parts(M, r) * n, of_xcd = on_xcd * parts(M, r);
+      if ((r == 256 && M <= 128) || (n > 1 && units > 1100)) continue;
+      const bool sets = r == 128 && units <= 256 && list > KT;
+      const double unit = r == 256 ? c.rows256 + c.tile256 * tiles : sets ? c.sets + c.tile_sets * (double)(((int64_t)tiles + 1) >> 1) : c.rows128 + c.tile128 * tiles;
+      look_at(r, 0, n, sets ? 2 : 1, both(unit * rounds((double)of_xcd, r == 256 || sets ? 32 : 64, c.ceil_rows), list_us));
+    }
   }
   // packed, as the beams of one request (offsets inside its rows fit 32 bits)
-  if (p->prefix_L > 0 && p->B > 1 && all < ((int64_t)1 << 22) && all * p->Hkv * p->d < ((int64_t)1 << 31)) {
+  if (M <= 80 && p->prefix_L > 0 && p->B > 1 && all < ((int64_t)1 << 22) && all * p->Hkv * p->d < ((int64_t)1 << 31)) {
     const double packed_us = (p->prefix_L + (double)p->max_L * p->B) * token_bytes / c.rate;
     for (const int n0 : {1, 2, 3, 4, 6, 8, 12, 16}) {
       if (n0 > 1 && n0 * 96 > p->prefix_L) break;
@@ -148,25 +161,25 @@ PagedPlan plan_fp4(const gr_attn_paged_params* p) {
       }
     }
   }
-  plan.find = plan.rows == 128 && plan.ks == 1 && pairs * plan.ns[1] > 256 && p->B >= 2 && p->B <= kRankB;
+  plan.find = plan.rows >= 128 && plan.ks == 1 && pairs * parts(M, plan.rows) * plan.ns[1] > 256 && p->B >= 2 && p->B <= kRankB;
   return plan;
 }
 
 PagedPlan plan_paged(const gr_attn_paged_params* p) {
+  if (p->kv_type == GR_KV_FP4) return plan_fp4(p);
   PagedPlan plan{};
   const int64_t g = p->Hq / p->Hkv, M = p->W * g, all = p->B * M, pairs = (int64_t)p->B * p->Hkv;
-  const bool kv8 = p->kv_type == GR_KV_FP8, kv4 = p->kv_type == GR_KV_FP4;
+  const bool kv8 = p->kv_type == GR_KV_FP8;
   auto parts = [](int64_t n, int64_t of) { return (n + of - 1) / of; };
   if (M > 80) {
     gr_attn_params q{};
     q.B = p->B; q.W = p->W; q.Hq = p->Hq; q.Hkv = p->Hkv; q.d = p->d; q.max_L = p->prefix_L + p->max_L;
     q.total_L = (int64_t)q.B * q.max_L;                      // (the lengths are on the GPU)
-    const AttnPlan a = plan_attn(&q, kv8 || kv4);
+    const AttnPlan a = plan_attn(&q, kv8);
     plan.rows = a.mwg; plan.ns[1] = a.nsplit; plan.ks = a.ks;
     plan.find = a.many && a.ks == 1 && p->B >= 2 && p->B <= kRankB;
     return plan;
   }
-  if (kv4) return plan_fp4(p);
   const PagedCost& c = kPagedCost[p->d == 128][kv8];
   const double partial_us = 2.0 * p->B * p->W * p->Hq * p->d * 4 / 2.7e6, token_bytes = 2.0 * p->Hkv * p->d * (kv8 ? 1 : 2);
   constexpr int kCounts[] = {1, 2, 3, 4, 6, 8, 12, 16};

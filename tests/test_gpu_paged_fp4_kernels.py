@@ -12,19 +12,19 @@ from test_code_objects import LLVM, code_objects  # noqa: F401  (the fixture)
 LONG = 70 * 64 + 21                          # tokens in more than 64 pages of 64
 # rows of a workgroup, packed prefix, sets of wavefronts, longest request first: requests, beams, heads, prefix, own tokens, pages inside a tile and of whole ones
 CASES = {
-    (256, False, 1, True): dict(lens=[LONG] + [(53 * b) % 300 for b in range(64)], W=128, Hq=8, Hkv=4, P=128, u=2, pages=(32, 64)),
-    (256, False, 1, False): dict(lens=[(53 * b) % 300 for b in range(128)] + [LONG], W=128, Hq=4, Hkv=2, P=0, u=1, pages=(16, 128)),
-    (128, False, 1, True): dict(lens=[130, LONG] + [(71 * b) % 400 for b in range(68)], W=41, Hq=8, Hkv=4, P=0, u=3, pages=(16, 64)),
-    (128, False, 1, False): dict(lens=[(29 * b) % 200 for b in range(128)] + [LONG], W=41, Hq=8, Hkv=4, P=256, u=1, pages=(32, 64)),
-    (128, False, 2, False): dict(lens=[2 * LONG] + [(71 * b) % 400 for b in range(63)], W=60, Hq=8, Hkv=4, P=0, u=2, pages=(16, 64)),
-    (16, False, 1, False): dict(lens=[LONG] + [(29 * b) % 200 for b in range(99)], W=3, Hq=16, Hkv=8, P=0, u=2, pages=(16, 64)),
-    (16, False, 2, False): dict(lens=[2 * LONG] + [(29 * b) % 200 for b in range(19)], W=3, Hq=8, Hkv=4, P=0, u=2, pages=(16, 64)),
-    (32, False, 1, False): dict(lens=[LONG] + [(29 * b) % 200 for b in range(99)], W=10, Hq=16, Hkv=8, P=0, u=2, pages=(16, 64)),
-    (32, False, 2, False): dict(lens=[2 * LONG] + [(29 * b) % 200 for b in range(19)], W=10, Hq=8, Hkv=4, P=0, u=2, pages=(16, 64)),
-    (16, True, 1, False): dict(lens=[LONG // 2] + [(17 * b) % 150 for b in range(127)], W=4, Hq=16, Hkv=4, P=6400, u=2, pages=(16, 64)),
-    (32, True, 1, False): dict(lens=[LONG // 2] + [(17 * b) % 150 for b in range(127)], W=8, Hq=16, Hkv=4, P=6400, u=2, pages=(16, 64)),
+    (256, False, 1, True): dict(lens=[LONG] + [(53 * b) % 300 for b in range(64)], W=41, Hq=16, Hkv=4, P=6400, u=2, pages=(32, 64)),
+    (256, False, 1, False): dict(lens=[(53 * b) % 300 for b in range(128)] + [LONG], W=41, Hq=8, Hkv=2, P=6400, u=1, pages=(16, 128)),
+    (128, False, 1, True): dict(lens=[130, LONG] + [(71 * b) % 400 for b in range(63)], W=50, Hq=4, Hkv=2, P=0, u=3, pages=(16, 64)),
+    (128, False, 1, False): dict(lens=[(29 * b) % 200 for b in range(128)] + [LONG], W=50, Hq=4, Hkv=2, P=0, u=1, pages=(32, 64)),
+    (128, False, 2, False): dict(lens=[LONG] + [(71 * b) % 400 for b in range(19)], W=50, Hq=4, Hkv=2, P=0, u=2, pages=(16, 64)),
+    (16, False, 1, False): dict(lens=[LONG // 2] + [(29 * b) % 200 for b in range(99)], W=2, Hq=8, Hkv=8, P=0, u=2, pages=(16, 64)),
+    (16, False, 2, False): dict(lens=[LONG] + [(29 * b) % 200 for b in range(19)], W=2, Hq=4, Hkv=2, P=0, u=2, pages=(16, 64)),
+    (32, False, 1, False): dict(lens=[LONG] + [(29 * b) % 200 for b in range(64)], W=10, Hq=4, Hkv=2, P=0, u=2, pages=(16, 64)),
+    (32, False, 2, False): dict(lens=[LONG] + [(29 * b) % 200 for b in range(19)], W=10, Hq=4, Hkv=2, P=0, u=2, pages=(16, 64)),
+    (16, True, 1, False): dict(lens=[LONG] + [(17 * b) % 150 for b in range(19)], W=2, Hq=8, Hkv=4, P=6400, u=2, pages=(16, 64)),
+    (32, True, 1, False): dict(lens=[LONG] + [(17 * b) % 150 for b in range(19)], W=10, Hq=8, Hkv=4, P=6400, u=2, pages=(16, 64)),
 }
-SPLIT = [dict(lens=[3000, 70, 1501], W=60, Hq=8, Hkv=4, P=128, u=2, pages=(16, 64)), dict(lens=[3000, 70, 1501], W=5, Hq=8, Hkv=4, P=128, u=2, pages=(16, 64)),
+SPLIT = [dict(lens=[3000, 70, 1501], W=100, Hq=8, Hkv=4, P=128, u=2, pages=(16, 64)), dict(lens=[5000, 70, 1501], W=200, Hq=16, Hkv=4, P=0, u=2, pages=(16, 64)), dict(lens=[3000, 70, 1501], W=5, Hq=8, Hkv=4, P=128, u=2, pages=(16, 64)),
          dict(lens=[3000, 70, 1501], W=12, Hq=8, Hkv=4, P=0, u=2, pages=(16, 64))]
 
 
