@@ -14,7 +14,7 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 // 16 * NB rows of a (request, KV head) pair against a segment of its keys.  The wavefronts hold the same rows and take 32 tokens each in turn; nobody waits for
 // anybody until their (maximum, sum, O) are joined in LDS.
-// Bound: memory (17/32 byte an element).  us: 64 requests of 14208 tokens x 1 beam, 32 and 8 heads of 128, 170 (5.8 TB/s; a plain read of 1 GiB reaches 6.3), 32 of 12001-16384 x 2, whose 256
+// Bound: memory (17/32 byte an element).  us: 64 requests of 14208 tokens x 1 beam, 32 and 8 heads of 128, 170-175 (5.7 TB/s; a plain read of 1 GiB reaches 6.3), 32 of 12001-16384 x 2, whose 256
 // workgroups end with the longest list, 94 (5.2); the same loads without anything done to what they bring 87.  Vector instructions (160 for a tile of one block) keep the SIMDs busy 37 % of that time.
 // Tried: the operands of V kept in order behind scheduling barriers 96.4 instead of 93.9; two tiles on their way instead of one 96-104; 128 registers for four wavefronts to a SIMD, with spills, 100-159; V asked for ahead of K 102; the powers of K and V in one load,
 // spread by ds_bpermute, 95 (and 3 % more where the loads are not waited for); 48 rows a wavefront, for many rows, 482 against 495 with 32 and 309 with gr_beam_attn's body.

@@ -348,7 +348,7 @@ extern "C" gr_status gr_qk_norm_rope(const gr_qk_norm_rope_params* p, void* stre
   if (p->T < 0 || p->Hq < 0 || p->Hkv < 0 || (has_q && p->Hq == 0) || ((has_k || has_v) && p->Hkv == 0)) return GR_ERR_INVALID_ARG;
   if (!has_q && !has_k && p->T > 0) return GR_ERR_INVALID_ARG;
   if (has_q != (p->q_out != nullptr) || has_k != (p->k_out != nullptr) || has_v != (p->v_out != nullptr)) return GR_ERR_INVALID_ARG;
-  if ((p->q_weight && !has_q) || (p->k_weight && !has_k)) return GR_ERR_INVALID_ARG;
+  if (p->T > 0 && ((p->q_weight && !has_q) || (p->k_weight && !has_k))) return GR_ERR_INVALID_ARG;         // (tensors of no rows may have no address)
   if (const gr_status st = turn_ok(p->d, p->rot, p->pairs, p->n_pos, p->eps, p->q_weight || p->k_weight, p->table, p->pos, p->T)) return st;
   const int64_t nq = (int64_t)p->Hq * p->d, nk = (int64_t)p->Hkv * p->d;
   if ((has_q && (p->q_stride < nq || p->q_out_stride < nq)) || (has_k && (p->k_stride < nk || p->k_out_stride < nk)) || (has_v && (p->v_stride < nk || p->v_out_stride < nk)))

@@ -139,6 +139,8 @@ def test_no_rows():
     empty = torch.zeros((0, 4, 64), dtype=torch.bfloat16, device=DEV)
     q, k = gr.gr_qk_norm_rope(empty, empty[:, :1], torch.zeros(0, dtype=torch.int32, device=DEV), table_of(4, 64).to(DEV))
     assert q.shape == (0, 4, 64) and k.shape == (0, 1, 64)
+    w = torch.ones(64, device=DEV)
+    assert gr.gr_qk_norm_rope(empty, empty, q_weight=w, k_weight=w)[1].shape == (0, 4, 64)
 
 
 def test_far_rows_and_strides():

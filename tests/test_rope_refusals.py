@@ -29,7 +29,8 @@ GOOD_READ = dict(T=10, Hkv=2, d=64, page_size=16, n_pages=64, kv_type=2, k_scale
     (dict(T=2 ** 31), -2), (dict(Hq=2 ** 15, q_stride=2 ** 21, q_out_stride=2 ** 21), -2), (dict(T=2 ** 31 - 1, Hq=256, q_stride=2 ** 14, q_out_stride=2 ** 14), -2),
     (dict(Hq=1, d=272, rot=16, q_stride=1024, q_out_stride=1024, k_stride=1024, k_out_stride=1024, v_stride=1024, v_out_stride=1024), -2),
     (dict(T=0), 0), (dict(T=0, q=None, q_out=None, q_weight=None), 0), (dict(T=0, k=None, k_out=None, k_weight=None, v=None, v_out=None), 0), (dict(T=0, rot=0, table=None, pos=None, n_pos=0), 0),
-    (dict(T=0, q_out=A, k_out=2 * A), 0), (dict(T=0, k=None, k_out=None, k_weight=None), 0)])
+    (dict(T=0, q_out=A, k_out=2 * A), 0), (dict(T=0, k=None, k_out=None, k_weight=None), 0),
+    (dict(T=0, q=None, q_out=None, k=None, k_out=None, v=None, v_out=None), 0), (dict(T=0, q=None, q_out=None, eps=-1.0), -1)])
 def test_norm_rope(gr, change, status):  # noqa: F811
     assert gr.load_library().gr_qk_norm_rope(ctypes.byref(ROPE(**{**GOOD_ROPE, **change})), None) == status
 
