@@ -287,7 +287,8 @@ gr_status gr_beam_attn_slots(const gr_attn_params* p, const int32_t* slot, void*
  * gr_qk_norm_rope - queries and keys of T rows on their way from a projection to attention: every head normed by itself and rotated by the row's position.
  *     y = x * w / sqrt(mean(x^2) + eps)                                 (q_weight, k_weight; NULL: y = x)
  *     y_a' = y_a cos - y_b sin,  y_b' = y_b cos + y_a sin               for i < rot / 2, (a, b) = (i, i + rot / 2), or with pairs = 1 (2 i, 2 i + 1)
- * with cos = table[pos, i], sin = table[pos, rot / 2 + i]; elements from rot on are not rotated.  In fp32, rounded to bf16 once.  Rows lie any strides apart: parts of a fused
+ * with cos = table[pos, i], sin = table[pos, rot / 2 + i]; elements from rot on are not rotated.  In fp32, rounded to bf16 once (so with eps = 0 a mean square
+ * has to be at least 2^-126, and a sum of squares below 2^128: of a larger one the finite elements come back as 0).  Rows lie any strides apart: parts of a fused
  * projection's rows, and the beams' own caches (a row's KV heads at k_unshared + ((b * W + w) * ND + token) * Hkv * d: a stride of ND * Hkv * d).  Queries or keys may be absent (NULL
  * with their output).  v, which is only moved to v_out beside the keys, is for such caches and may be absent too.  With rot > 0 rows whose position is outside [0, n_pos) are left as they
  * were in all outputs.  q_out is q itself (same stride), or does not overlap any input; so is k_out with k; v_out overlaps nothing.

@@ -396,7 +396,8 @@ def gr_page_write(k, v, slot, k_pages, v_pages, k_scale=1.0, v_scale=1.0, stream
 def gr_qk_norm_rope(q, k, pos=None, table=None, q_weight=None, k_weight=None, eps=1e-6, pairs=False, q_out=None, k_out=None, v=None, v_out=None, stream=None):
     """Queries and keys normed head by head and rotated.  q bf16 [T,Hq,d], k bf16 [T,Hkv,d] (either may be None): rows contiguous and any stride apart, as are q_out and k_out (new
     tensors where they are None; the inputs themselves: in place).  q_weight, k_weight fp32 [d]: the norms' weights (None: not normed).  table fp32 [n_pos,rot]: rot/2 cosines, then
-    rot/2 sines of every position (None: not rotated), pos int32 [T]; rows whose position is outside the table are left as they were.  pairs: element 2i turns with 2i+1 instead of
+    rot/2 sines of every position (None: not rotated), pos int32 [T]; rows whose position is outside the table are left as they were (new
+    tensors: whatever is there).  pairs: element 2i turns with 2i+1 instead of
     i with i + rot/2.  v, v_out [T,Hkv,d]: values that are moved beside the keys.  Returns (q_out, k_out).  Enqueues on `stream`."""
     native = _native or _marshal()
     if q_out is None and q is not None:

@@ -135,6 +135,14 @@ def test_zeros_infinities_and_nan_stay_in_their_heads():
     assert torch.isnan(zero).all()                         # 0 / 0, as the formula has it
 
 
+def test_squares_beyond_a_float():
+    """128 squares of 2^126 pass 2^128: 0.  Those of 2^120 do not: the formula's 1, a unit of fp32 or two off, which is 1 in bf16."""
+    x = torch.full((2, 1, 128), 2.0 ** 63, dtype=torch.bfloat16)
+    x[1] = 2.0 ** 60
+    y, _ = gr.gr_qk_norm_rope(x.to(DEV), None, q_weight=torch.ones(128, device=DEV))
+    assert (y[0] == 0).all() and (y[1] == 1).all()
+
+
 def test_no_rows():
     empty = torch.zeros((0, 4, 64), dtype=torch.bfloat16, device=DEV)
     q, k = gr.gr_qk_norm_rope(empty, empty[:, :1], torch.zeros(0, dtype=torch.int32, device=DEV), table_of(4, 64).to(DEV))
