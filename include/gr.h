@@ -288,7 +288,9 @@ gr_status gr_beam_attn_slots(const gr_attn_params* p, const int32_t* slot, void*
  *     y = x * w / sqrt(mean(x^2) + eps)                                 (q_weight, k_weight; NULL: y = x)
  *     y_a' = y_a cos - y_b sin,  y_b' = y_b cos + y_a sin               for i < rot / 2, (a, b) = (i, i + rot / 2), or with pairs = 1 (2 i, 2 i + 1)
  * with cos = table[pos, i], sin = table[pos, rot / 2 + i]; elements from rot on are not rotated.  In fp32, rounded to bf16 once (so with eps = 0 a mean square
- * has to be at least 2^-126, and a sum of squares below 2^128: of a larger one the finite elements come back as 0).  Rows lie any strides apart: parts of a fused
+ * has to be at least 2^-126, and a sum of squares below 2^128: of a larger one the finite elements come back as 0).  Before that every operation is rounded to nearest by itself: the sum of the
+ * squares (neighbours first: where d and rot are powers of two fours in a chain, of d up to 64 in pairs, then pairs of neighbouring sums), times 1 / d, plus eps, the reciprocal root, x times that,
+ * times w; two products, their difference or sum.  Rows lie any strides apart: parts of a fused
  * projection's rows, and the beams' own caches (a row's KV heads at k_unshared + ((b * W + w) * ND + token) * Hkv * d: a stride of ND * Hkv * d).  Queries or keys may be absent (NULL
  * with their output).  v, which is only moved to v_out beside the keys, is for such caches and may be absent too.  With rot > 0 rows whose position is outside [0, n_pos) are left as they
  * were in all outputs.  q_out is q itself (same stride), or does not overlap any input; so is k_out with k; v_out overlaps nothing.
@@ -391,7 +393,8 @@ gr_status gr_page_write(const gr_page_write_params* p, void* stream);
  * rotated), in fp32 and rounded once, to the pool's type.  Values go as they are.  Rows whose slot is outside [0, n_pages * page_size) or, with rot > 0, whose position is outside
  * [0, n_pos) are not written; a slot that two rows have holds either's elements, in parts too (GR_KV_FP4: codes of one may stand under scales of the other).  GR_KV_FP8: codes as gr_page_write makes them (of rotated or normed keys the quotient
  * may be one unit of fp32 off the division's).  GR_KV_FP4: a block's scale is the smallest power of two, from 2^-120 to 2^125, with |x| <= 7 * scale for its 32 values (no value is
- * further off than half the distance of the codes around it); codes are the nearest, ties to even.  Only enqueues on `stream`.  The pools do not overlap k, v or each other.
+ * further off than half the distance of the codes around it); codes are the nearest, ties to even, to the values in fp32 (of normed or rotated keys, whose exact values may lie a few units of
+ * fp32 away, on the other side of the border between two codes).  Only enqueues on `stream`.  The pools do not overlap k, v or each other.
  * Supported: d a multiple of 16 (GR_KV_FP4: 32) up to 256; rot a multiple of 16 up to d; Hkv * d at most 2^20; the strides multiples of 8; T and n_pages * page_size below
  * 2^31.  k, v, the pools, k_weight and table 16-byte aligned.  Errors: INVALID_ARG, UNSUPPORTED, HIP. */
 typedef struct {

@@ -3,6 +3,10 @@
 // A head x of d elements is normed, y = x w / sqrt(mean(x^2) + eps), and its first `rot` elements are turned in pairs by the angles of the row's position,
 //     y_a' = y_a cos - y_b sin,   y_b' = y_b cos + y_a sin,
 // with (a, b) = (i, i + rot / 2) or (2 i, 2 i + 1) for i < rot / 2.  All of it is in fp32; the only rounding to fewer bits is the store's.
+// A code of FP4 is a whole step away from its neighbours, so that next to a border the last bit of an fp32 value decides between values that are far apart.  So every operation is rounded by
+// itself (this file is compiled without contraction), in the order in which the formulas read: the squares' sum by neighbours (fours in a chain, of heads up to 64 in pairs, then pairs of
+// sums), times 1 / d, plus eps, its reciprocal root rounded to nearest, x times that, times w; two products, then their difference or sum.  A plain evaluation in fp32, operation by operation,
+// has the same bits.  (With r w first, another order of sums and fused rotations 14 to 22 of the 134 million codes of 32 x 4096 keys of 8 x 128 were others than that evaluation's.)
 //
 // Bound: memory, 4 bytes an element in and out (bf16).  A lane holds 16 elements of a head in two runs of eight, so that both of every pair are its own: elements 8 j .. and
 // rot / 2 + 8 j .., or 16 j .. .  4, 8 or 16 lanes hold the head, and a wavefront the same head of 16, 8 or 4 consecutive rows: what it writes into an FP4 page is then one
@@ -20,18 +24,36 @@ __device__ __forceinline__ unsigned div_by(unsigned n, unsigned d, uint32_t inv)
   return q + (n - q * d >= d ? 1u : 0u);
 }
 
-// Sum and maximum over groups of LG neighbouring lanes, in all of them.
+// Of a neighbouring lane
 template <int CTRL>
 __device__ __forceinline__ float lanes_of(float v) {
   return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, 0xf, 0xf, false));
 }
-template <int LG>
-__device__ __forceinline__ float group_sum(float v) {
-  v += lanes_of<0xb1>(v);                        // lane ^ 1
-  v += lanes_of<0x4e>(v);                        // lane ^ 2
-  if (LG >= 8) v += lanes_of<0x141>(v);          // the other four of eight (in reverse, but they are alike)
-  if (LG >= 16) v += lanes_of<0x140>(v);
-  return v;
+// Sum of a head's squares; a and b: those of a lane's two runs of eight.  Whatever the lane layout, neighbouring eights meet first, then neighbouring pairs of them, and so on: where the first
+// `split` lanes hold runs that lie apart, the sums of the two are kept apart until one run of all of them is whole (rot / 16 a power of two; for other numbers of lanes the order is another).
+template <int LG, bool PAIRS>
+__device__ __forceinline__ float head_sum(float a, float b, int split, bool apart) {
+  a += PAIRS || !apart ? b : 0.f;
+  b = PAIRS || !apart ? 0.f : b;
+  auto meet = [&](int lanes, auto of) __attribute__((always_inline)) {
+    if (!PAIRS && split == lanes) { a += b; b = 0.f; }
+    a += of(a);
+    if (!PAIRS) b += of(b);
+  };
+  meet(1, [](float v) { return lanes_of<0xb1>(v); });                   // lane ^ 1
+  meet(2, [](float v) { return lanes_of<0x4e>(v); });                   // lane ^ 2
+  if (LG >= 8) meet(4, [](float v) { return lanes_of<0x141>(v); });     // the other four of eight (in reverse, but they are alike)
+  if (LG >= 16) meet(8, [](float v) { return lanes_of<0x140>(v); });
+  return PAIRS ? a : a + b;
+}
+
+// 1 / sqrt(x) rounded to nearest (for all 2^25 significands and parities of the exponent): the instruction's, a unit of fp32 off at most, and two terms of the root's series around it in
+// 64 bits.  Of 0, infinities and NaN the instruction's.
+__device__ __forceinline__ float reciprocal_root(float x) {
+  const float r = __builtin_amdgcn_rsqf(x);
+  const double e = __builtin_fma(-((double)x * (double)r), (double)r, 1.0);          // (the first product is exact)
+  const float y = (float)__builtin_fma((double)r * e, __builtin_fma(0.375, e, 0.5), (double)r);
+  return __builtin_fabs(e) < 1.0 ? y : r;
 }
 
 struct TurnCtx {
@@ -117,21 +139,24 @@ __device__ __forceinline__ void turned(float (&y)[16], const Head& h, const Angl
   h.numbers(y);
   ws.of(weight, p);
   if (weight) {
-    float sum = 0.f;
+    auto eight = [&](const float* v) __attribute__((always_inline)) {        // (squares of bf16 values are exact in fp32: nothing is lost or won by adding them in one instruction)
+      auto four = [](const float* v) __attribute__((always_inline)) {
+        return LG == 4 ? fmaf(v[1], v[1], v[0] * v[0]) + fmaf(v[3], v[3], v[2] * v[2]) : fmaf(v[3], v[3], fmaf(v[2], v[2], fmaf(v[1], v[1], v[0] * v[0])));
+      };
+      return four(v) + four(v + 4);
+    };
+    const float sum = head_sum<LG, PAIRS>(p.holds ? eight(y) : 0.f, p.holds ? eight(y + 8) : 0.f, c.rot >> 4, p.turns && c.rot > 16);
+    const float r = reciprocal_root(sum * c.inv_d + c.eps);
 #pragma unroll
-    for (int e = 0; e < 16; e++) sum = fmaf(y[e], y[e], sum);
-    sum = group_sum<LG>(p.holds ? sum : 0.f);
-    const float r = __builtin_amdgcn_rsqf(fmaf(sum, c.inv_d, c.eps));
-#pragma unroll
-    for (int e = 0; e < 16; e++) y[e] *= r * ws.w[e];
+    for (int e = 0; e < 16; e++) y[e] = y[e] * r * ws.w[e];
   }
   if (p.turns) {
 #pragma unroll
     for (int k = 0; k < 8; k++) {
       const int i = PAIRS ? 2 * k : k, j = PAIRS ? 2 * k + 1 : k + 8;
       const float u = y[i], v = y[j];
-      y[i] = fmaf(u, a.cs[k], -(v * a.sn[k]));
-      y[j] = fmaf(v, a.cs[k], u * a.sn[k]);
+      y[i] = u * a.cs[k] - v * a.sn[k];
+      y[j] = v * a.cs[k] + u * a.sn[k];
     }
   }
 }
