@@ -293,7 +293,7 @@ gr_status gr_beam_attn_slots(const gr_attn_params* p, const int32_t* slot, void*
  * times w; two products, their difference or sum.  Rows lie any strides apart: parts of a fused
  * projection's rows, and the beams' own caches (a row's KV heads at k_unshared + ((b * W + w) * ND + token) * Hkv * d: a stride of ND * Hkv * d).  Queries or keys may be absent (NULL
  * with their output).  v, which is only moved to v_out beside the keys, is for such caches and may be absent too.  With rot > 0 rows whose position is outside [0, n_pos) are left as they
- * were in all outputs.  q_out is q itself (same stride), or does not overlap any input; so is k_out with k; v_out overlaps nothing.
+ * were in all outputs.  q_out is q itself (same stride), or does not overlap any input; so is k_out with k; v_out overlaps nothing (an output that begins where another tensor does is refused).
  * Only enqueues on `stream`.  Supported: d a multiple of 16 up to 256; rot a multiple of 16 up to d (0: no rotation; pos and table are not looked at); Hq * d and Hkv * d at most
  * 2^20; strides multiples of 8; T < 2^31.  All tensors but pos 16-byte aligned.  Errors: INVALID_ARG, UNSUPPORTED, HIP.
  * ------------------------------------------------------------------------------------------------ */

@@ -344,6 +344,8 @@ extern "C" gr_status gr_page_read(const gr_page_read_params* p, void* stream_) {
   const int64_t n = (int64_t)p->Hkv * p->d;
   if (!p->k_pages || !p->v_pages) return GR_ERR_INVALID_ARG;
   if (p->T > 0 && (!p->k || !p->v || !p->slot || p->k == p->v)) return GR_ERR_INVALID_ARG;
+  for (const void* out : {p->k, p->v})
+    if (out && (out == p->k_pages || out == p->v_pages || out == p->slot)) return GR_ERR_INVALID_ARG;
   if (p->k_stride < n || p->v_stride < n) return GR_ERR_INVALID_ARG;
   if (((uintptr_t)p->k | (uintptr_t)p->v | (uintptr_t)p->k_pages | (uintptr_t)p->v_pages) & 15 || ((uintptr_t)p->slot & 3)) return GR_ERR_INVALID_ARG;
   if (!gr_page_size_ok(p->page_size) || p->d % 16 || p->d > 256 || p->k_stride % 8 || p->v_stride % 8 || n > 1 << 20) return GR_ERR_UNSUPPORTED;

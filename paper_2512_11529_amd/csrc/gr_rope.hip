@@ -331,6 +331,12 @@ bool any_misaligned(std::initializer_list<const void*> of, uintptr_t mask) {
   return false;
 }
 
+bool is_one_of(const void* out, std::initializer_list<const void*> of) {
+  for (const void* p : of)
+    if (out && out == p) return true;
+  return false;
+}
+
 // What both calls ask of a rotation and of a head's size
 gr_status turn_ok(int32_t d, int32_t rot, int32_t pairs, int32_t n_pos, float eps, bool norms, const float* table, const int32_t* pos, int64_t T) {
   if (d <= 0 || rot < 0 || rot > d || (pairs != 0 && pairs != 1)) return GR_ERR_INVALID_ARG;
@@ -379,8 +385,9 @@ extern "C" gr_status gr_qk_norm_rope(const gr_qk_norm_rope_params* p, void* stre
   if ((has_q && (p->q_stride < nq || p->q_out_stride < nq)) || (has_k && (p->k_stride < nk || p->k_out_stride < nk)) || (has_v && (p->v_stride < nk || p->v_out_stride < nk)))
     return GR_ERR_INVALID_ARG;
   if ((p->q_out == p->q && has_q && p->q_out_stride != p->q_stride) || (p->k_out == p->k && has_k && p->k_out_stride != p->k_stride)) return GR_ERR_INVALID_ARG;
-  if (has_v && (p->v_out == p->v || p->v_out == p->k_out || p->v_out == p->q_out)) return GR_ERR_INVALID_ARG;
-  if (has_q && has_k && p->q_out == p->k_out) return GR_ERR_INVALID_ARG;
+  if (is_one_of(p->q_out, {p->k, p->v, p->q_weight, p->k_weight, p->table, p->pos, p->k_out, p->v_out}) || is_one_of(p->k_out, {p->q, p->v, p->q_weight, p->k_weight, p->table, p->pos, p->v_out}) ||
+      is_one_of(p->v_out, {p->q, p->k, p->v, p->q_weight, p->k_weight, p->table, p->pos}))
+    return GR_ERR_INVALID_ARG;                               // (other wavefronts would read rows that are written over already)
   if (any_misaligned({p->q, p->k, p->v, p->q_weight, p->k_weight, p->table, p->q_out, p->k_out, p->v_out}, 15) || any_misaligned({p->pos}, 3)) return GR_ERR_INVALID_ARG;
   auto odd = [](bool has, int64_t a, int64_t b) { return has && (a % 8 || b % 8); };
   if (odd(has_q, p->q_stride, p->q_out_stride) || odd(has_k, p->k_stride, p->k_out_stride) || odd(has_v, p->v_stride, p->v_out_stride)) return GR_ERR_UNSUPPORTED;
@@ -416,6 +423,8 @@ extern "C" gr_status gr_page_append(const gr_page_append_params* p, void* stream
   if (p->kv_type != GR_KV_BF16 && p->kv_type != GR_KV_FP8 && p->kv_type != GR_KV_FP4) return GR_ERR_INVALID_ARG;
   if (p->kv_type == GR_KV_FP8 && (!gr_scale_ok(p->k_scale) || !gr_scale_ok(p->v_scale))) return GR_ERR_INVALID_ARG;
   if (!p->k_pages || !p->v_pages || p->k_pages == p->v_pages) return GR_ERR_INVALID_ARG;
+  for (const void* pool : {p->k_pages, p->v_pages})
+    if (is_one_of(pool, {p->k, p->v, p->slot, p->pos, p->table, p->k_weight})) return GR_ERR_INVALID_ARG;
   if (p->T > 0 && (!p->k || !p->v || !p->slot)) return GR_ERR_INVALID_ARG;
   if (const gr_status st = turn_ok(p->d, p->rot, p->pairs, p->n_pos, p->eps, p->k_weight != nullptr, p->table, p->pos, p->T)) return st;
   const int64_t n = (int64_t)p->Hkv * p->d;
