@@ -415,19 +415,20 @@ def kv_fp4_page_bytes(page_size, d) -> int:
     return int(load_library().gr_kv_fp4_page_bytes(int(page_size), int(d)))
 
 
-def gr_page_append(k, v, slot, k_pages, v_pages, pos=None, table=None, k_weight=None, eps=1e-6, pairs=False, k_scale=1.0, v_scale=1.0, stream=None):
+def gr_page_append(k, v, slot, k_pages, v_pages, pos=None, table=None, k_weight=None, eps=1e-6, pairs=False, k_scale=1.0, v_scale=1.0, stream=None, page_size=None):
     """K/V rows into their slots, the keys normed (k_weight) and rotated (pos, table, pairs) as by gr_qk_norm_rope on the way.  k, v, slot as for gr_page_write; k_pages, v_pages
     [n_pages,page_size,Hkv,d] in bf16 or uint8 (E4M3 codes of x / scale), or uint8 [n_pages,Hkv,kv_fp4_page_bytes(page_size,d)] for FP4.  Rows whose slot is outside the pool or whose
-    position is outside the table are not written.  Enqueues on `stream`."""
-    rc = (_native or _marshal()).page_append(k, v, slot, k_pages, v_pages, pos, table, k_weight, eps, pairs, k_scale, v_scale, stream)
+    position is outside the table are not written.  page_size: a ValueError where the pages are of another (the bytes of FP4 pages do not say whose they are: 16 tokens of heads of 128
+    are as many as 32 of 64).  Enqueues on `stream`."""
+    rc = (_native or _marshal()).page_append(k, v, slot, k_pages, v_pages, pos, table, k_weight, eps, pairs, k_scale, v_scale, page_size, stream)
     if rc != 0:
         raise GrError(rc, "gr_page_append")
 
 
-def gr_page_read(k_pages, v_pages, slot, k, v, k_scale=1.0, v_scale=1.0, stream=None):
+def gr_page_read(k_pages, v_pages, slot, k, v, k_scale=1.0, v_scale=1.0, stream=None, page_size=None):
     """The rows in slots `slot` int32 [T] of pools of any type into k, v bf16 [T,Hkv,d] (rows contiguous and any stride apart); rows whose slot is outside the pool are left as they
-    were.  Returns (k, v).  Enqueues on `stream`."""
-    rc = (_native or _marshal()).page_read(k_pages, v_pages, slot, k, v, k_scale, v_scale, stream)
+    were.  page_size: as for gr_page_append.  Returns (k, v).  Enqueues on `stream`."""
+    rc = (_native or _marshal()).page_read(k_pages, v_pages, slot, k, v, k_scale, v_scale, page_size, stream)
     if rc != 0:
         raise GrError(rc, "gr_page_read")
     return k, v
@@ -449,18 +450,18 @@ def _paged_shapes(B, W, Hq, Hkv, d, max_L, prefix_L, fp8, page_size, fp4=False):
 
 
 def gr_beam_attn_paged(q, k_pages, v_pages, block_table, seq_lens, k_unshared, v_unshared, u, sm_scale, max_L, prefix_pages=None, prefix_L=0, k_scale=1.0,
-                       v_scale=1.0, slot=None, out=None, lse_out=None, workspace=None, stream=None):
+                       v_scale=1.0, slot=None, out=None, lse_out=None, workspace=None, stream=None, page_size=None):
     """Beam attention over a prompt cache in pages.  q bf16 [B,W,Hq,d]; k/v_pages [n_pages,page_size,Hkv,d], bf16 or uint8 (E4M3 codes, value = code * scale),
     or uint8 [n_pages,Hkv,kv_fp4_page_bytes(page_size,d)] (FP4); block_table int32 [B,max_pages]; seq_lens int32 [B]; k/v_unshared bf16 [B,W,ND,Hkv,d] (None: no own tokens, u = 0); `slot` as for gr_beam_attn_slots.
     prefix_pages int32 [prefix_L/page_size]: pages of the tokens in front that all requests share.  max_L (the largest of seq_lens, or more) and prefix_L are host
-    integers.  Returns (out bf16 [B,W,Hq,d], lse fp32 [B,W,Hq] or None).  Enqueues on `stream` (default: current)."""
+    integers.  page_size: as for gr_page_append.  Returns (out bf16 [B,W,Hq,d], lse fp32 [B,W,Hq] or None).  Enqueues on `stream` (default: current)."""
     native = _native or _marshal()
     if out is None:
         out = _empty(q.shape, "bfloat16", q.device, stream)
     args = (q, k_pages, v_pages, block_table, seq_lens, k_unshared, v_unshared, u, sm_scale, max_L, prefix_pages, prefix_L, k_scale, v_scale, slot, out, lse_out)
-    rc = native.attn_paged(*args, workspace, stream)
+    rc = native.attn_paged(*args, workspace, page_size, stream)
     if rc > 0:                                   # no workspace was given: so many bytes are needed
-        rc = native.attn_paged(*args, _scratch(rc, q.device, stream), stream)
+        rc = native.attn_paged(*args, _scratch(rc, q.device, stream), page_size, stream)
     if rc != 0:
         raise GrError(rc, "gr_beam_attn_paged")
     return out, lse_out

@@ -370,28 +370,40 @@ PyObject* page_write(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// A pool of any type for heads of size d: uint8 [n_pages, Hkv, bytes] is FP4, uint8 [n_pages, page_size, Hkv, d] FP8, bf16 of that shape bf16.
+// A pool of any type for heads of size d: uint8 [n_pages, Hkv, bytes] is FP4, uint8 [n_pages, page_size, Hkv, d] FP8, bf16 of that shape bf16.  page_size: None, or what its pages are to hold (the
+// bytes of FP4 pages do not say by themselves of what head size they are: 16 tokens of 128 are as many as 32 of 64).
 struct Pool {
   int32_t kv_type;
   int64_t pages, page, Hkv;
   at::ScalarType type;
   const at::Tensor* t;
 };
-Pool any_pool(PyObject* o, const char* name, int64_t d) {
+Pool any_pool(PyObject* o, const char* name, int64_t d, PyObject* page_size) {
   const at::Tensor* t = THPVariable_Check(o) ? &THPVariable_Unpack(o) : nullptr;
-  if (!(t && t->scalar_type() == at::kByte && t->dim() == 3)) {
+  const bool fp4 = t && t->scalar_type() == at::kByte && t->dim() == 3;
+  Pool p;
+  if (!fp4) {
     bool fp8;
     t = &pool(o, name, &fp8);
-    return {fp8 ? GR_KV_FP8 : GR_KV_BF16, t->size(0), t->size(1), t->size(2), fp8 ? at::kByte : at::kBFloat16, t};
+    p = {fp8 ? GR_KV_FP8 : GR_KV_BF16, t->size(0), t->size(1), t->size(2), fp8 ? at::kByte : at::kBFloat16, t};
+  } else {
+    t = &tensor_nd(o, at::kByte, name, 3);
+    const int64_t bytes = t->size(2), page = d > 0 && d % 32 == 0 ? bytes / (d / 2 + d / 32) : 0;
+    if (page == 0 || page * (d / 2 + d / 32) != bytes) {
+      PyErr_Format(PyExc_ValueError, "%s: expected pages of %lld bytes a token and KV head (head size %lld in FP4), got shape %s", name, (long long)(d / 2 + d / 32), (long long)d,
+                   shape_text(t->sizes()).c_str());
+      throw Error();
+    }
+    p = {GR_KV_FP4, t->size(0), page, t->size(1), at::kByte, t};
   }
-  t = &tensor_nd(o, at::kByte, name, 3);
-  const int64_t bytes = t->size(2), page = d > 0 && d % 32 == 0 ? bytes / (d / 2 + d / 32) : 0;
-  if (page == 0 || page * (d / 2 + d / 32) != bytes) {
-    PyErr_Format(PyExc_ValueError, "%s: expected pages of %lld bytes a token and KV head (head size %lld in FP4), got shape %s", name, (long long)(d / 2 + d / 32), (long long)d,
-                 shape_text(t->sizes()).c_str());
-    throw Error();
+  if (page_size != Py_None) {
+    const long long want = integer(page_size);
+    if (want != p.page) {
+      PyErr_Format(PyExc_ValueError, "%s: expected pages of %lld tokens, got %lld (head size %lld) of shape %s", name, want, (long long)p.page, (long long)d, shape_text(t->sizes()).c_str());
+      throw Error();
+    }
   }
-  return {GR_KV_FP4, t->size(0), page, t->size(1), at::kByte, t};
+  return p;
 }
 // Optional tensors, each on the call's GPU
 void* given_on(OnDevice& on, PyObject* o, at::ScalarType type, const char* name, c10::IntArrayRef shape) {
@@ -452,10 +464,10 @@ PyObject* norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// page_append(k, v, slot, k_pages, v_pages, pos | None, table | None, k_weight | None, eps, pairs, k_scale, v_scale, stream) -> status
+// page_append(k, v, slot, k_pages, v_pages, pos | None, table | None, k_weight | None, eps, pairs, k_scale, v_scale, page_size | None, stream) -> status
 PyObject* page_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded([&]() -> PyObject* {
-    count(n, 13);
+    count(n, 14);
     OnDevice on;
     const at::Tensor* k;
     rows_of(a[0], "k", &k);
@@ -463,7 +475,7 @@ PyObject* page_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     gr_page_append_params p{};
     p.k = rows_given(on, a[0], "k", {T, Hkv, d}, &p.k_stride);
     p.v = rows_given(on, a[1], "v", {T, Hkv, d}, &p.v_stride);
-    const Pool kp = any_pool(a[3], "k_pages", d);
+    const Pool kp = any_pool(a[3], "k_pages", d, a[12]);
     if (kp.kv_type == GR_KV_FP4) tensor(a[3], kp.type, "k_pages", {kp.pages, Hkv, kp.t->size(2)});
     else tensor(a[3], kp.type, "k_pages", {kp.pages, kp.page, Hkv, d});
     p.k_pages = given_on(on, a[3], kp.type, "k_pages", kp.t->sizes());
@@ -479,15 +491,15 @@ PyObject* page_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     p.k_weight = (const float*)given_on(on, a[7], at::kFloat, "k_weight", {d});
     p.T = T; p.Hkv = int32_of(Hkv, "k"); p.d = int32_of(d, "k"); p.page_size = int32_of(kp.page, "k_pages"); p.n_pages = int32_of(kp.pages, "k_pages"); p.kv_type = kp.kv_type;
     p.eps = (float)real(a[8]); p.pairs = truth(a[9]); p.k_scale = (float)real(a[10]); p.v_scale = (float)real(a[11]);
-    void* stream = on.stream(a[12]);
+    void* stream = on.stream(a[13]);
     return status_of([&] { return p_page_append(&p, stream); });
   });
 }
 
-// page_read(k_pages, v_pages, slot, k, v, k_scale, v_scale, stream) -> status
+// page_read(k_pages, v_pages, slot, k, v, k_scale, v_scale, page_size | None, stream) -> status
 PyObject* page_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded([&]() -> PyObject* {
-    count(n, 8);
+    count(n, 9);
     OnDevice on;
     const at::Tensor* k;
     rows_of(a[3], "k", &k);
@@ -495,7 +507,7 @@ PyObject* page_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
     gr_page_read_params p{};
     p.k = rows_given(on, a[3], "k", {T, Hkv, d}, &p.k_stride);
     p.v = rows_given(on, a[4], "v", {T, Hkv, d}, &p.v_stride);
-    const Pool kp = any_pool(a[0], "k_pages", d);
+    const Pool kp = any_pool(a[0], "k_pages", d, a[7]);
     if (kp.kv_type == GR_KV_FP4) tensor(a[0], kp.type, "k_pages", {kp.pages, Hkv, kp.t->size(2)});
     else tensor(a[0], kp.type, "k_pages", {kp.pages, kp.page, Hkv, d});
     p.k_pages = given_on(on, a[0], kp.type, "k_pages", kp.t->sizes());
@@ -503,16 +515,16 @@ PyObject* page_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
     p.slot = (const int32_t*)given_on(on, a[2], at::kInt, "slot", {T});
     p.T = T; p.Hkv = int32_of(Hkv, "k"); p.d = int32_of(d, "k"); p.page_size = int32_of(kp.page, "k_pages"); p.n_pages = int32_of(kp.pages, "k_pages"); p.kv_type = kp.kv_type;
     p.k_scale = (float)real(a[5]); p.v_scale = (float)real(a[6]);
-    void* stream = on.stream(a[7]);
+    void* stream = on.stream(a[8]);
     return status_of([&] { return p_page_read(&p, stream); });
   });
 }
 
 // attn_paged(q, k_pages, v_pages, block_table, seq_lens, k_own | None, v_own | None, u, sm_scale, max_L, prefix_pages | None, prefix_L, k_scale, v_scale,
-//            slot | None, out, lse | None, workspace | None, stream) -> status (<= 0), or the workspace bytes that the call needs when none was given
+//            slot | None, out, lse | None, workspace | None, page_size | None, stream) -> status (<= 0), or the workspace bytes that the call needs when none was given
 PyObject* attn_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded([&]() -> PyObject* {
-    count(n, 19);
+    count(n, 20);
     OnDevice on;
     const at::Tensor& q = tensor_nd(a[0], at::kBFloat16, "q", 4);
     on.add("q", q);
@@ -523,7 +535,7 @@ PyObject* attn_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
       on.add(name, t);
       return t.data_ptr();
     };
-    const Pool kp = any_pool(a[1], "k_pages", d);
+    const Pool kp = any_pool(a[1], "k_pages", d, a[18]);
     const int64_t pages = kp.pages, page = kp.page, Hkv = kp.Hkv;
     if (kp.kv_type != GR_KV_FP4) tensor(a[1], kp.type, "k_pages", {pages, page, Hkv, d});
     gr_attn_paged_params p{};
@@ -549,7 +561,7 @@ PyObject* attn_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
     size_t ws_bytes;
     void* ws = const_cast<void*>(any_tensor(a[17], &ws_bytes));
     if (a[17] != Py_None) on.add("workspace", THPVariable_Unpack(a[17]));
-    void* stream = on.stream(a[18]);
+    void* stream = on.stream(a[19]);
     if (a[17] == Py_None) {
       const size_t need = p_attn_paged_ws(&p);
       if (need > 0) return workspace_wanted(need);
