@@ -393,7 +393,7 @@ gr_status gr_page_write(const gr_page_write_params* p, void* stream);
  * rotated), in fp32 and rounded once, to the pool's type.  Values go as they are.  Rows whose slot is outside [0, n_pages * page_size) or, with rot > 0, whose position is outside
  * [0, n_pos) are not written; a slot that two rows have holds either's elements, in parts too (GR_KV_FP4: codes of one may stand under scales of the other).  GR_KV_FP8: codes as gr_page_write makes them (of rotated or normed keys the quotient
  * may be one unit of fp32 off the division's).  GR_KV_FP4: a block's scale is the smallest power of two, from 2^-120 to 2^125, with |x| <= 7 * scale for its 32 values (no value is
- * further off than half the distance of the codes around it); codes are the nearest, ties to even, to the values in fp32 (of normed or rotated keys, whose exact values may lie a few units of
+ * further off than half the distance of the codes around it), and 2^125 where a finite one is above 7 * 2^125 (all of those become 6 * 2^125, up to two steps off); codes are the nearest, ties to even, to the values in fp32 (of normed or rotated keys, whose exact values may lie a few units of
  * fp32 away, on the other side of the border between two codes).  Only enqueues on `stream`.  The pools do not overlap k, v or each other.
  * Supported: d a multiple of 16 (GR_KV_FP4: 32) up to 256; rot a multiple of 16 up to d; Hkv * d at most 2^20; the strides multiples of 8; T and n_pages * page_size below
  * 2^31.  k, v, the pools, k_weight and table 16-byte aligned.  Errors: INVALID_ARG, UNSUPPORTED, HIP. */
@@ -440,7 +440,9 @@ gr_status gr_page_read(const gr_page_read_params* p, void* stream);
  * prefix is read and multiplied once for the rows of all requests; with more, each request's rows meet it by themselves.
  * What a table holds beyond a request's pages is of no effect; a page number outside [0, n_pages) is read as page 0, and a length outside [0, max_L] as the
  * nearer end.  Slots of a page behind a request's last token may hold anything.
- * GR_KV_FP8: pools of E4M3 codes, scales applied as in gr_beam_attn_fp8kv.  GR_KV_FP4: codes are widened with their blocks' scales to bf16, exactly (scales 2^-120 to 2^125).
+ * GR_KV_FP8: pools of E4M3 codes, scales applied as in gr_beam_attn_fp8kv.  GR_KV_FP4: codes are widened with their blocks' scales to bf16, exactly (scale bytes 7 to 252).
+ * A block with the scale byte 255 (gr_page_append made it of an infinite value or NaN) is no finite value: of a row with such a key or value any result may come, finite ones too, and not
+ * always NaN; gr_page_read shows such blocks.
  * Supported: d in {64, 128}; Hq % Hkv == 0; 0 <= u <= ND; prefix_L a multiple of page_size; n_pages * page_size below 2^31, and that times
  * Hkv * d below 2^41; prefix_L + max_L below 2^30; Hkv * d <= 65536; W * Hq/Hkv < 2^22.  bf16 tensors and pools 16-byte aligned; finite values in the slots that are read; |v| * 2^8 * (number of keys) below 2^128.
  * Workspace (device, 256-byte aligned, contents unspecified before and after): partial results of segments, where a row's keys are split.

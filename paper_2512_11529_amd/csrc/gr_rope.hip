@@ -237,7 +237,7 @@ struct AppendCtx {
 };
 
 // FP4: the scale of 32 values is the smallest power of two 2^e, -120 <= e <= 125, with |y| <= 7 * 2^e, so that no value is further from its code's than half the distance of the two
-// codes around it (the largest is 6, 7 half a step above it; with 2^(floor(log2 max) - 2), the usual choice, values between 7 and 8 are up to a whole step off).  `most`: the bits of the
+// codes around it (the largest is 6, 7 half a step above it; with 2^(floor(log2 max) - 2), the usual choice, values between 7 and 8 are up to a whole step off).  Finite values above 7 * 2^125 have no such power: they are cut to 6 * 2^125.  `most`: the bits of the
 // largest, of which 1.75 * 2^k + 0x1fffff are the last that keep their exponent.
 __device__ __forceinline__ uint32_t fp4_power(uint32_t most) { return min(max((most + 0x1fffffu) >> 23, 9u) - 2u, 252u); }
 // Eight values as codes under the scale 2^(power - 127), to nearest, ties to even
