@@ -17,7 +17,7 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 // Bound: memory (17/32 byte an element).  us: 64 requests of 14208 tokens x 1 beam, 32 and 8 heads of 128, 170-175 (5.7 TB/s; a plain read of 1 GiB reaches 6.3), 32 of 12001-16384 x 2, whose 256
 // workgroups end with the longest list, 94 (5.2); the same loads without anything done to what they bring 87.  Vector instructions (160 for a tile of one block) keep the SIMDs busy 37 % of that time.
 // Tried: the operands of V kept in order behind scheduling barriers 96.4 instead of 93.9; two tiles on their way instead of one 96-104; 128 registers for four wavefronts to a SIMD, with spills, 100-159; V asked for ahead of K 102; the powers of K and V in one load,
-// spread by ds_bpermute, 95 (and 3 % more where the loads are not waited for); 48 rows a wavefront, for many rows, 482 against 495 with 32 and 309 with gr_beam_attn's body.
+// spread by ds_bpermute, 95 (and 3 % more where the loads are not waited for); 48 rows a wavefront, for many rows, 482 against 495 with 32.
 template <int D>
 struct Fp4 {
   static constexpr int FT = 32;                    // tokens of a tile: two halves of 16
@@ -354,7 +354,7 @@ __global__ void __launch_bounds__(WAVES * 64) __attribute__((amdgpu_waves_per_eu
 }
 
 // Blocks of 128 and 256 rows: gr_beam_attn's body, bound as it is by the issue rate of matrix instructions, softmax and LDS reads: 32 requests of 512-3700 tokens x 256 beams behind 256, 32 and 8
-// heads of 128, 309-318 us (1.05 PFLOP/s; bf16 pages 313-324).  By blocks of 32 rows whose wavefronts share out the keys 495; with the powers looked at where they are asked for 333.
+// heads of 128, 309-328 us from card to card (1.01-1.08 PFLOP/s; bf16 pages 313-324); heads of 64 201 (0.83).  By blocks of 32 rows whose wavefronts share out the keys 495; with the powers looked at where they are asked for 333.
 template <int D, int NWAVES, int KS, bool FIND>
 __global__ void __launch_bounds__(NWAVES * 64 * KS) __attribute__((amdgpu_waves_per_eu(2, 2))) k_fp4_attn(AttnCtx c) {
   constexpr int NCB = 1;

@@ -5,14 +5,16 @@
 // with (a, b) = (i, i + rot / 2) or (2 i, 2 i + 1) for i < rot / 2.  All of it is in fp32; the only rounding to fewer bits is the store's.
 // A code of FP4 is a whole step away from its neighbours, so that next to a border the last bit of an fp32 value decides between values that are far apart.  So every operation is rounded by
 // itself (this file is compiled without contraction), in the order in which the formulas read: the squares' sum by neighbours (fours in a chain, of heads up to 64 in pairs, then pairs of
-// sums), times 1 / d, plus eps, its reciprocal root rounded to nearest, x times that, times w; two products, then their difference or sum.  A plain evaluation in fp32, operation by operation,
+// sums: any order will do, and this is how a mean over the last axis in plain torch operations adds heads of 64 and 128), times 1 / d, plus eps, its reciprocal root rounded to nearest, x times that, times w; two products, then their difference or sum.  A plain evaluation in fp32, operation by operation,
 // has the same bits.  (With r w first, another order of sums and fused rotations 14 to 22 of the 134 million codes of 32 x 4096 keys of 8 x 128 were others than that evaluation's.)
 //
 // Bound: memory, 4 bytes an element in and out (bf16).  A lane holds 16 elements of a head in two runs of eight, so that both of every pair are its own: elements 8 j .. and
 // rot / 2 + 8 j .., or 16 j .. .  4, 8 or 16 lanes hold the head, and a wavefront the same head of 16, 8 or 4 consecutive rows: what it writes into an FP4 page is then one
 // run of codes and one of scales, and a lane's cosines and sines serve all of its heads.  The wavefronts of a workgroup take different heads of the same rows.
-// With 16 consecutive elements a lane and the other halves of its pairs loaded a second time, 32 x 256 rows of 32 + 8 + 8 heads of 128, normed, took 69.6 us, now 40.9 (4.9 TB/s; a copy of
-// 1 GiB reaches 5.15), 32 x 4096 tokens of 8 heads into FP4 361 us, now 146 (4.7).  The launch is all there is of 16 rows of 8 + 8 + 8 heads of 64: 2.7 us.
+// With 16 consecutive elements a lane and the other halves of its pairs loaded a second time, 32 x 256 rows of 32 + 8 + 8 heads of 128, normed, took 69.6 us, now 41.4 (4.9 TB/s; a copy of
+// 1 GiB reaches 5.15), 32 x 4096 tokens of 8 heads into FP4 361 us, now 147 (4.7; bf16 216, 5.0, FP8 163, 5.0; heads of 64 4.4-4.8).  The launch is all there is of 16 rows of 8 + 8 + 8
+// heads of 64: 2.8 us.  16 prompts of 60-700 tokens of 8 heads into FP8 take 10.1 us, 7.5 without norm and rotation: all wavefronts are resident at once, and each waits for one chain of loads,
+// position, angles, and the rows and weights behind them, those that hold only heads of V too, which need no angles.
 #include <initializer_list>
 #include <type_traits>
 #include "gr_pages.hpp"
@@ -355,6 +357,8 @@ unsigned grid_of(TurnCtx* t, int lg, int heads, int per_wave) {
   const int64_t rows = 64 / lg, grid = ((int64_t)t->T + rows - 1) / rows * t->chunks;
   return gr_grid_fits(grid, 256) ? (unsigned)grid : 0;
 }
+// (Head sizes between powers of two leave lanes without work: 67000 rows of 8 heads into bf16 pages, d = 80 85 us, 96 91, 160 139, 208 183, 4.0 to 4.9 TB/s; gr_page_write, which has no heads,
+// 71, 82, 135, 174.  Of 64, 128, 192 and 256 both take the same.)
 int lanes_of_head(int d) { return d <= 64 ? 4 : d <= 128 ? 8 : 16; }
 
 template <class F>
@@ -362,7 +366,8 @@ gr_status with_lanes(int lg, F&& f) {
   return lg == 4 ? f(std::integral_constant<int, 4>()) : lg == 8 ? f(std::integral_constant<int, 8>()) : f(std::integral_constant<int, 16>());
 }
 // Heads of a wavefront: four, which share their angles and the norm's weights, once the launch fills the chip so (4096 wavefronts, four to a SIMD).  us with one and with four: prompts
-// of 36 thousand tokens, 32 and 8 heads of 128, 153.7, 142.7; 32 x 4096 tokens of 8 heads into FP4 (and back) 310, 290; 16 prompts of 60-700 tokens into FP8 9.9, 10.4.
+// of 36 thousand tokens, 32 and 8 heads of 128, 154.9, 143.9; 32 x 4096 tokens of 8 heads into FP4 (and back) 298.7, 282.3; 32 x 256 rows of 32 + 8 + 8 heads 42.0, 41.7; 16 prompts of
+// 60-700 tokens into FP8 10.8, 11.0.
 template <class F>
 gr_status with_heads(int64_t T, int lg, int heads, F&& f) {
   const int64_t waves = (T + 64 / lg - 1) / (64 / lg) * heads;
