@@ -5,8 +5,9 @@
 // with (a, b) = (i, i + rot / 2) or (2 i, 2 i + 1) for i < rot / 2.  All of it is in fp32; the only rounding to fewer bits is the store's.
 // A code of FP4 is a whole step away from its neighbours, so that next to a border the last bit of an fp32 value decides between values that are far apart.  So every operation is rounded by
 // itself (this file is compiled without contraction), in the order in which the formulas read: the squares' sum by neighbours (fours in a chain, of heads up to 64 in pairs, then pairs of
-// sums: any order will do, and this is how a mean over the last axis in plain torch operations adds heads of 64 and 128), times 1 / d, plus eps, its reciprocal root rounded to nearest, x times that, times w; two products, then their difference or sum.  A plain evaluation in fp32, operation by operation,
-// has the same bits.  (With r w first, another order of sums and fused rotations 14 to 22 of the 134 million codes of 32 x 4096 keys of 8 x 128 were others than that evaluation's.)
+// sums: any order will do, and this is how a mean over the last axis in plain torch operations adds heads of 64 and 128), times 1 / d, plus eps, its reciprocal root rounded to nearest, x times
+// that, times w; two products, then their difference or sum.  A plain evaluation in fp32, operation by operation, has the same bits.  (With r w first, another order of sums and fused
+// rotations 14 to 22 of the 134 million codes of 32 x 4096 keys of 8 x 128 were others than that evaluation's.)
 //
 // Bound: memory, 4 bytes an element in and out (bf16).  A lane holds 16 elements of a head in two runs of eight, so that both of every pair are its own: elements 8 j .. and
 // rot / 2 + 8 j .., or 16 j .. .  4, 8 or 16 lanes hold the head, and a wavefront the same head of 16, 8 or 4 consecutive rows: what it writes into an FP4 page is then one
